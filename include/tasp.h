@@ -39,8 +39,8 @@ typedef enum tasp_status {
   TASP_ENOMEM = -7             /* host allocation failed */
 } tasp_status;
 
-enum { TASP_MASK_FULL = 0, TASP_MASK_ZIGZAG_CAUSAL = 1 };
-enum { TASP_DTYPE_FP32 = 0, TASP_DTYPE_BF16 = 1 };
+enum { TASP_MASK_FULL = 0, TASP_MASK_ZIGZAG_CAUSAL = 1, TASP_MASK_CAUSAL = 2 /* paged cache only */ };
+enum { TASP_DTYPE_FP32 = 0, TASP_DTYPE_BF16 = 1, TASP_DTYPE_E4M3 = 2 /* paged cache only */ };
 enum { TASP_ORDER_TASP = 0, TASP_ORDER_RING = 1 };
 
 /* Human-readable text for a status code (static storage, never NULL). */
@@ -360,6 +360,96 @@ int tasp_chunk_attn_bwd_profile(const tasp_schedule_t* s, const tasp_attn_bwd_ar
 /* Algorithmic work of one backward call: five products against the forward's two, i.e. 2.5 times
  * tasp_chunk_attn_flops (the recomputation of the scores in both kernels is not counted). */
 double tasp_chunk_attn_bwd_flops(const tasp_schedule_t* s, const tasp_attn_bwd_args* a);
+
+/* ----------------------------------------------------------------------------------------------
+ * A paged cache of K and V, and the attention of new tokens over it.               [device work]
+ *
+ * The serving side of the computation above: a prompt's K and V are kept in pages, tokens are added one
+ * by one or in chunks and attend to all of their sequence.  tasp_cache_write puts dense rows into the
+ * pages, tasp_cache_read takes rows out (what tasp_chunk_attn reads), tasp_paged_attn attends over the
+ * pages; with TASP_MASK_FULL and fp32 outputs its pair (out, lse) is one part of a sequence whose cache
+ * is spread over ranks, and tasp_lse_merge / tasp_lse_merge_many join the parts.
+ *
+ * The pages (tasp_paged_cache; all device pointers, 16-byte aligned):
+ *   k, v      [n_pages, Hkv, page_size, d]: a head's rows of a page lie together.  page_size a power of
+ *             two from 16 to 1024, d 64 or 128.
+ *   dtype     TASP_DTYPE_BF16, or TASP_DTYPE_E4M3 (8-bit floats without infinities, largest value 448).
+ *   k_scale,  [n_pages, Hkv, page_size] bytes, TASP_DTYPE_E4M3 only: byte b of a row stands for the factor
+ *   v_scale   2^(b - 127) of its d values (b = 0: 0).
+ *
+ * The batch (tasp_paged_batch; the three lists are device memory, 4-byte aligned, read when the kernels run):
+ *   row_start [n_seqs + 1]  not falling; rows row_start[b] .. row_start[b+1] - 1 of the dense tensors are
+ *             the last tokens of sequence b.  n_rows is the number of rows of the dense tensors.
+ *   kv_len    [n_seqs]  tokens of the sequence, those rows included.  With n rows, row j of a sequence has
+ *             position kv_len - n + j.
+ *   page_table [n_seqs, max_pages]  position t lies in slot t % page_size of page page_table[b][t / page_size].
+ *             An entry outside [0, n_pages) names no page: nothing is written there, rows read from there are
+ *             0 and its keys are not visible.  Neither are positions below 0.
+ *   max_rows  the most rows of any sequence, or 0 if it is not known: it decides only which kernel runs.
+ * Whatever the lists hold, no access leaves the buffers that the arguments describe: row_start is clipped to
+ * [0, n_rows] and kv_len to [0, max_pages * page_size].  Rows of the dense outputs outside
+ * [row_start[0], row_start[n_seqs]) are left as they are.  A page may be in several tables (shared
+ * prefixes); a position that two rows write in one call holds either, or parts of both.
+ * max_pages * page_size <= 2^30, n_rows <= 2^30 (with tasp_paged_attn n_rows * Hq / Hkv <= 2^30).
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct tasp_paged_cache {
+  void*    k;
+  void*    v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int64_t  n_pages;
+  int32_t  page_size, Hkv, d, dtype;
+} tasp_paged_cache;
+
+typedef struct tasp_paged_batch {
+  const int32_t* page_table;
+  const int32_t* kv_len;
+  const int32_t* row_start;
+  int64_t        n_rows;
+  int32_t        n_seqs, max_pages, max_rows;
+} tasp_paged_batch;
+
+/* Rows of k and v (device, [n_rows, Hkv, d] of `dtype` fp32 or bf16, 16-byte aligned; k_stride and v_stride
+ * elements from one row to the next, a multiple of 8, 0 for dense) go to their places in the pages.  bf16 pages:
+ * rounded to nearest even.  e4m3 pages: the row of a head is stored as its values over 2^e, rounded to nearest even,
+ * with the smallest integer e >= -100 for which the largest finite magnitude is at most 448 2^e; infinities and NaN are
+ * stored as NaN, magnitudes above 1.875 2^127 as that. */
+int tasp_cache_write(const tasp_paged_cache* c, const tasp_paged_batch* b, const void* k, const void* v,
+                     int64_t k_stride, int64_t v_stride, int32_t dtype, void* hip_stream);
+
+/* The other way: every row of k and v (device, dense [n_rows, Hkv, d] of `dtype`) from its place in the
+ * pages, times its scale.  Exact in both types. */
+int tasp_cache_read(const tasp_paged_cache* c, const tasp_paged_batch* b, void* k, void* v, int32_t dtype,
+                    void* hip_stream);
+
+/* Attention of the rows of q over the pages of their sequences.
+ *   q         device, [n_rows, Hq, d] bf16, q_stride elements from one token to the next (a multiple of 8, 0 for
+ *             dense).  Query head h reads KV head h*Hkv/Hq.
+ *   out, lse  device, dense [n_rows, Hq, d] of out_dtype (bf16, or fp32 for a part that is merged) and [n_rows, Hq] fp32:
+ *             as in tasp_chunk_attn.  A row that sees no key gets out = 0, lse = -inf.
+ *   mask_mode TASP_MASK_CAUSAL: key t is visible to position p iff t <= p; TASP_MASK_FULL: every token of the sequence
+ *             is (its kv_len may then be less than its rows, or 0).
+ *   window,   TASP_MASK_CAUSAL with window W > 0: of those keys the last W (t > p - W) and the first `sinks`
+ *   sinks     (t < sinks).  0: all.
+ *   softmax_scale  0 means 1/sqrt(d); otherwise positive and finite.
+ *   workspace device, >= tasp_paged_attn_workspace_bytes() bytes, 256-byte aligned, caller-owned, contents undefined on
+ *             entry and exit; calls that may overlap need one each.
+ * Infinities and NaN in keys or values that a row does not see do not reach it.  K, V and P are multiplied in bf16
+ * and summed in fp32.  The call only enqueues kernels on hip_stream and may be recorded into a graph; results
+ * depend on the lists and inputs alone. */
+typedef struct tasp_paged_attn_args {
+  const void* q;
+  void*       out;
+  float*      lse;
+  void*       workspace;
+  size_t      workspace_bytes;
+  int64_t     q_stride;
+  int32_t     Hq, out_dtype, mask_mode, window, sinks;
+  float       softmax_scale;
+} tasp_paged_attn_args;
+
+size_t tasp_paged_attn_workspace_bytes(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_paged_attn_args* a);
+int    tasp_paged_attn(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_paged_attn_args* a, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -16,8 +16,8 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtasp.so")
 
-MASK_FULL, MASK_ZIGZAG_CAUSAL = 0, 1
-DTYPE_FP32, DTYPE_BF16 = 0, 1
+MASK_FULL, MASK_ZIGZAG_CAUSAL, MASK_CAUSAL = 0, 1, 2
+DTYPE_FP32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
 ORDER_TASP, ORDER_RING = 0, 1
 
 OK, EINVAL, EUNSUPPORTED_N, EUNSUPPORTED_SHAPE, EALIGN, EWORKSPACE, EHIP, ENOMEM = 0, -1, -2, -3, -4, -5, -6, -7
@@ -32,7 +32,8 @@ EXPORTS = [
     "tasp_lse_merge_many", "tasp_calibration_mfma", "tasp_calibration_issue", "tasp_schedule_create_multinode",
     "tasp_chunk_attn_bwd_workspace_bytes", "tasp_chunk_attn_bwd", "tasp_chunk_attn_bwd_profile",
     "tasp_chunk_attn_bwd_flops", "tasp_chunk_attn_static", "tasp_chunk_attn_best_workspace_bytes",
-    "tasp_chunk_attn_bwd_best_workspace_bytes",
+    "tasp_chunk_attn_bwd_best_workspace_bytes", "tasp_cache_write", "tasp_cache_read", "tasp_paged_attn_workspace_bytes",
+    "tasp_paged_attn",
 ]
 STATIC_SCRATCH_BYTES = 64 << 20
 
@@ -73,6 +74,22 @@ class AttnBwdArgs(C.Structure):
 class BwdProfile(C.Structure):
     _fields_ = [("dq_ms", C.c_double), ("dkv_ms", C.c_double), ("other_ms", C.c_double),
                 ("dq_launches", C.c_int32), ("dkv_launches", C.c_int32), ("other_launches", C.c_int32)]
+
+
+class PagedCacheArgs(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int64),
+                ("page_size", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32)]
+
+
+class PagedBatchArgs(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("row_start", C.c_void_p), ("n_rows", C.c_int64),
+                ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("max_rows", C.c_int32)]
+
+
+class PagedAttnArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("q_stride", C.c_int64), ("Hq", C.c_int32), ("out_dtype", C.c_int32), ("mask_mode", C.c_int32), ("window", C.c_int32),
+                ("sinks", C.c_int32), ("softmax_scale", C.c_float)]
 
 
 def _load():
@@ -126,6 +143,12 @@ def _load():
     lib.tasp_chunk_attn_bwd_profile.argtypes = [C.c_void_p, C.POINTER(AttnBwdArgs), C.c_void_p, C.POINTER(BwdProfile)]
     lib.tasp_chunk_attn_bwd_flops.argtypes = [C.c_void_p, C.POINTER(AttnBwdArgs)]
     lib.tasp_chunk_attn_bwd_flops.restype = C.c_double
+    paged = [C.POINTER(PagedCacheArgs), C.POINTER(PagedBatchArgs)]
+    lib.tasp_cache_write.argtypes = paged + [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p]
+    lib.tasp_cache_read.argtypes = paged + [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+    lib.tasp_paged_attn_workspace_bytes.argtypes = paged + [C.POINTER(PagedAttnArgs)]
+    lib.tasp_paged_attn_workspace_bytes.restype = C.c_size_t
+    lib.tasp_paged_attn.argtypes = paged + [C.POINTER(PagedAttnArgs), C.c_void_p]
     return lib
 
 
@@ -409,3 +432,176 @@ def tasp_lse_merge(o_acc, lse_acc, o_part, lse_part):
     _check(lib.tasp_lse_merge(o_acc.data_ptr(), lse_acc.data_ptr(), o_part.data_ptr(), lse_part.data_ptr(),
                               rows, heads, d, C.c_void_p(s)), "tasp_lse_merge")
     return o_acc, lse_acc
+
+
+_ROW_TYPES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+
+
+def _on_device(device, **tensors):
+    for name, t in tensors.items():
+        if not t.is_cuda:
+            raise ValueError("%s must be a device tensor" % name)
+        if t.device != device:
+            raise ValueError("%s is on %s, the cache on %s" % (name, t.device, device))
+
+
+def _rows(name, t, heads, d, n_rows, types):
+    """Checks rows [n_rows, heads, d] whose tokens may be any number of elements apart; returns that number."""
+    if t.dim() != 3 or tuple(t.shape) != (n_rows, heads, d) or t.dtype not in types:
+        raise ValueError("%s must be [%d, %d, %d] of %s" % (name, n_rows, heads, d, " or ".join(str(x) for x in types)))
+    if n_rows == 0 or t.is_contiguous():
+        return 0
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d) or (n_rows > 1 and t.stride(0) < heads * d):
+        raise ValueError("a token's heads in %s must be contiguous" % name)
+    return t.stride(0) if n_rows > 1 else 0
+
+
+class PagedCache:
+    """K and V in pages: k, v [n_pages, Hkv, page_size, d] in bfloat16, or in float8_e4m3fn with k_scale, v_scale [n_pages, Hkv,
+    page_size] in float8_e8m0fnu (powers of two).  Holds the tensors; they are the caller's."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4 or v.shape != k.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError("k, v must be [n_pages, Hkv, page_size, d] of torch.bfloat16 or torch.float8_e4m3fn")
+        held = {"k": k, "v": v}
+        if k.dtype == torch.float8_e4m3fn:
+            held.update(k_scale=k_scale, v_scale=v_scale)
+            for t in (k_scale, v_scale):
+                if t is None or t.shape != k.shape[:3] or t.dtype != torch.float8_e8m0fnu:
+                    raise ValueError("e4m3 pages need k_scale, v_scale [n_pages, Hkv, page_size] of torch.float8_e8m0fnu")
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("bfloat16 pages have no scales")
+        _on_device(k.device, **held)
+        for name, t in held.items():
+            if not t.is_contiguous():
+                raise ValueError("%s must be contiguous" % name)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.Hkv, self.page_size, self.d = k.shape
+        self.device = k.device
+        a = PagedCacheArgs()
+        a.k, a.v = k.data_ptr(), v.data_ptr()
+        if k_scale is not None:
+            a.k_scale, a.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+        a.n_pages, a.page_size, a.Hkv, a.d = self.n_pages, self.page_size, self.Hkv, self.d
+        a.dtype = DTYPE_BF16 if k.dtype == torch.bfloat16 else DTYPE_E4M3
+        self.args = a
+
+    @classmethod
+    def empty(cls, n_pages, page_size, Hkv, d, dtype=torch.bfloat16, device="cuda"):
+        """New pages, contents undefined."""
+        k, v = (torch.empty((n_pages, Hkv, page_size, d), dtype=dtype, device=device) for _ in range(2))
+        if dtype != torch.float8_e4m3fn:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty((n_pages, Hkv, page_size), dtype=torch.float8_e8m0fnu, device=device) for _ in range(2)))
+
+
+class PagedBatch:
+    """Sequences of a PagedCache, as int32 device tensors that are read when a call runs: page_table [n_seqs, max_pages], kv_len [n_seqs]
+    (tokens, the new rows included), row_start [n_seqs + 1] (first row of each sequence in the dense tensors).  n_rows: rows of the dense
+    tensors; max_rows: the most of any sequence, 0 if not known (a hint)."""
+
+    def __init__(self, page_table, kv_len, row_start, n_rows, max_rows=0):
+        if page_table.dim() != 2 or tuple(kv_len.shape) != (page_table.shape[0],) or tuple(row_start.shape) != (page_table.shape[0] + 1,):
+            raise ValueError("expected page_table [n_seqs, max_pages], kv_len [n_seqs] and row_start [n_seqs + 1]")
+        for name, t in (("page_table", page_table), ("kv_len", kv_len), ("row_start", row_start)):
+            if t.dtype != torch.int32 or not t.is_contiguous():
+                raise ValueError("%s must be a contiguous int32 tensor" % name)
+        _on_device(page_table.device, page_table=page_table, kv_len=kv_len, row_start=row_start)
+        self.page_table, self.kv_len, self.row_start, self.n_rows = page_table, kv_len, row_start, int(n_rows)
+        a = PagedBatchArgs()
+        a.page_table, a.kv_len, a.row_start = page_table.data_ptr(), kv_len.data_ptr(), row_start.data_ptr()
+        a.n_rows, a.n_seqs, a.max_pages, a.max_rows = self.n_rows, page_table.shape[0], page_table.shape[1], int(max_rows)
+        self.args = a
+
+
+class _PagedPlan:
+    """What the plans of a paged cache share: the device, and the stream of a run."""
+
+    def __init__(self, cache, batch):
+        _on_device(cache.device, page_table=batch.page_table)
+        self.cache, self.batch = cache, batch
+        self._c, self._b = C.byref(cache.args), C.byref(batch.args)
+
+    def _stream(self, stream):
+        if torch._C._cuda_getDevice() != self.cache.device.index:
+            raise ValueError("the cache is on %s, which is not the current device" % self.cache.device)
+        return _stream() if stream is None else stream
+
+
+class CacheWritePlan(_PagedPlan):
+    """tasp_cache_write of k, v [n_rows, Hkv, d] (float32 or bfloat16; tokens may be any number of elements apart)."""
+
+    def __init__(self, k, v, cache, batch):
+        super().__init__(cache, batch)
+        _on_device(cache.device, k=k, v=v)
+        self._strides = [_rows(name, t, cache.Hkv, cache.d, batch.n_rows, _ROW_TYPES) for name, t in (("k", k), ("v", v))]
+        if k.dtype != v.dtype:
+            raise ValueError("k, v must share a dtype")
+        self._dtype, self._keep = _ROW_TYPES[k.dtype], (k, v)
+        self._args = (self._c, self._b, k.data_ptr(), v.data_ptr(), *self._strides, self._dtype)
+
+    def run(self, stream=None):
+        s = self._stream(stream)
+        if self.batch.n_rows > 0:
+            _check(lib.tasp_cache_write(*self._args, s), "tasp_cache_write")
+        return self.cache
+
+
+def tasp_cache_write(k, v, cache, batch):
+    """Rows of k and v into their places in the cache's pages.  Returns the cache."""
+    return CacheWritePlan(k, v, cache, batch).run()
+
+
+class CacheReadPlan(_PagedPlan):
+    """tasp_cache_read into k, v [n_rows, Hkv, d] of its own."""
+
+    def __init__(self, cache, batch, dtype=torch.bfloat16):
+        super().__init__(cache, batch)
+        if dtype not in _ROW_TYPES:
+            raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+        self.k, self.v = (torch.empty((batch.n_rows, cache.Hkv, cache.d), dtype=dtype, device=cache.device) for _ in range(2))
+        self._args = (self._c, self._b, self.k.data_ptr(), self.v.data_ptr(), _ROW_TYPES[dtype])
+
+    def run(self, stream=None):
+        s = self._stream(stream)
+        if self.batch.n_rows > 0:
+            _check(lib.tasp_cache_read(*self._args, s), "tasp_cache_read")
+        return self.k, self.v
+
+
+def tasp_cache_read(cache, batch, dtype=torch.bfloat16):
+    """The batch's rows of K and V out of the pages: (k, v) [n_rows, Hkv, d] in float32 or bfloat16."""
+    return CacheReadPlan(cache, batch, dtype).run()
+
+
+class PagedAttnPlan(_PagedPlan):
+    """Buffers of one tasp_paged_attn shape (out, lse, workspace), so that repeated calls allocate nothing.  q [n_rows, Hq, d] in bfloat16
+    (tokens may be any number of elements apart); out_dtype bfloat16, or float32 for a part that is merged."""
+
+    def __init__(self, q, cache, batch, mask_mode=MASK_CAUSAL, window=0, sinks=0, softmax_scale=0.0, out_dtype=torch.bfloat16):
+        super().__init__(cache, batch)
+        _on_device(cache.device, q=q)
+        if q.dim() != 3 or out_dtype not in _ROW_TYPES:
+            raise ValueError("expected q [n_rows, Hq, d], and out_dtype torch.bfloat16 or torch.float32")
+        a = PagedAttnArgs()
+        a.q_stride = _rows("q", q, q.shape[1], cache.d, batch.n_rows, (torch.bfloat16,))
+        a.Hq, a.out_dtype, a.mask_mode, a.window, a.sinks, a.softmax_scale = q.shape[1], _ROW_TYPES[out_dtype], mask_mode, window, sinks, softmax_scale
+        self.out = torch.empty(q.shape, dtype=out_dtype, device=q.device)
+        self.lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        nbytes = lib.tasp_paged_attn_workspace_bytes(self._c, self._b, C.byref(a))
+        self.workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=q.device)
+        a.q, a.out, a.lse = q.data_ptr(), self.out.data_ptr(), self.lse.data_ptr()
+        a.workspace, a.workspace_bytes = self.workspace.data_ptr(), nbytes
+        self.args, self._keep = a, q
+        self._args = (self._c, self._b, C.byref(a))
+
+    def run(self, stream=None):
+        s = self._stream(stream)
+        if self.batch.n_rows > 0:
+            _check(lib.tasp_paged_attn(*self._args, s), "tasp_paged_attn")
+        return self.out, self.lse
+
+
+def tasp_paged_attn(q, cache, batch, mask_mode=MASK_CAUSAL, window=0, sinks=0, softmax_scale=0.0, out_dtype=torch.bfloat16):
+    """Attention of the batch's rows over the pages of their sequences.  Returns (out [n_rows, Hq, d], lse [n_rows, Hq] fp32)."""
+    return PagedAttnPlan(q, cache, batch, mask_mode, window, sinks, softmax_scale, out_dtype).run()
