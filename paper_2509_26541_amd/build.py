@@ -8,7 +8,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtasp.so")
 SOURCES = ["schedule.cpp", "attn_bf16.hip", "attn_tile.hip", "attn_run.hip", "attn_bwd_bf16.hip", "attn_bwd_fp32.hip", "merge.hip", "calib.hip", "api.hip",
-           "cache.hip", "attn_paged.hip", "api_paged.hip"]
+           "cache.hip", "attn_paged.hip", "attn_paged_tile.hip", "api_paged.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno-gpu-rdc",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -12,6 +12,7 @@
 namespace {
 
 using tasp::PagedView;
+using tasp::larger;
 
 constexpr int64_t kMost = int64_t{1} << 30;          // positions of a table, rows
 bool misaligned(const void* p, uintptr_t by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) != 0; }
@@ -27,6 +28,7 @@ int check_common(const tasp_paged_cache* c, const tasp_paged_batch* b, PagedView
   if (c->d != 64 && c->d != 128) return TASP_EUNSUPPORTED_SHAPE;
   if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0) return TASP_EUNSUPPORTED_SHAPE;
   if (c->n_pages > kMost || b->n_rows > kMost || static_cast<int64_t>(b->max_pages) * c->page_size > kMost) return TASP_EUNSUPPORTED_SHAPE;
+  if (static_cast<int64_t>(c->Hkv) * c->page_size * c->d * 2 >= (int64_t{1} << 31)) return TASP_EUNSUPPORTED_SHAPE;      // a page's bytes
   if (misaligned(c->k, 16) || misaligned(c->v, 16)) return TASP_EALIGN;
   if (e4m3 && (misaligned(c->k_scale, 16) || misaligned(c->v_scale, 16))) return TASP_EALIGN;
   if (misaligned(b->page_table, 4) || misaligned(b->kv_len, 4) || misaligned(b->row_start, 4)) return TASP_EALIGN;
@@ -53,6 +55,12 @@ int check_common(const tasp_paged_cache* c, const tasp_paged_batch* b, PagedView
 
 bool rows_type(int32_t dtype) { return dtype == TASP_DTYPE_FP32 || dtype == TASP_DTYPE_BF16; }
 int status_of(hipError_t e) { return e == hipSuccess ? TASP_OK : TASP_EHIP; }
+
+// Which kernel: up to 16 rows (token, query head of the group) the one that has 16, by the hint or the mean.
+bool few_rows(const tasp::PagedAttn& p, const tasp_paged_batch* b) {
+  const int64_t rows = b->max_rows > 0 ? b->max_rows : (b->n_rows + larger(b->n_seqs, 1) - 1) / larger(b->n_seqs, 1);
+  return rows * p.G <= 16;
+}
 
 int check_attn(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_paged_attn_args* a, tasp::PagedAttn* out) {
   tasp::PagedAttn p{};
@@ -118,7 +126,7 @@ int tasp_cache_read(const tasp_paged_cache* c, const tasp_paged_batch* b, void* 
 size_t tasp_paged_attn_workspace_bytes(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_paged_attn_args* a) {
   tasp::PagedAttn p;
   if (check_attn(c, b, a, &p) != TASP_OK) return 0;
-  return static_cast<size_t>(tasp::paged_rows_workspace(c->dtype == TASP_DTYPE_E4M3, c->d));
+  return static_cast<size_t>(few_rows(p, b) ? tasp::paged_rows_workspace(c->d) : tasp::paged_tile_workspace(c->d));
 }
 
 int tasp_paged_attn(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_paged_attn_args* a, void* hip_stream) {
@@ -133,7 +141,9 @@ int tasp_paged_attn(const tasp_paged_cache* c, const tasp_paged_batch* b, const 
     if (misaligned(a->workspace, 256)) return TASP_EALIGN;
   }
   if (p.c.n_rows == 0 || p.c.n_seqs == 0) return TASP_OK;
-  return status_of(tasp::launch_paged_rows(p, c->dtype == TASP_DTYPE_E4M3, c->d, static_cast<hipStream_t>(hip_stream)));
+  const bool e4m3 = c->dtype == TASP_DTYPE_E4M3;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return status_of(few_rows(p, b) ? tasp::launch_paged_rows(p, e4m3, c->d, stream) : tasp::launch_paged_tile(p, e4m3, c->d, stream));
 }
 
 }  // extern "C"

@@ -14,11 +14,9 @@
 // scores and the probabilities.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
-#include <climits>
-
 #include "internal.hpp"
 #include "paged.hpp"
+#include "paged_combine.hpp"
 #include "pipeline.hpp"
 
 namespace tasp {
@@ -55,24 +53,6 @@ __device__ __forceinline__ bf16x8 widen(u32x2 w) {
   return r.v;
 }
 
-// EL values from `col` on of the row (token, query head) at index rh: sums over their weights' total, and the log-sum-exp.
-template <int D, int EL>
-__device__ __forceinline__ void finish_row(const PagedAttn& p, int64_t rh, int col, const float (&acc)[EL], float top, float total) {
-  const bool none = total == 0.f;
-  const float inv = none ? 0.f : 1.f / total;
-  if (p.out_fp32) {
-    float* const dst = static_cast<float*>(p.out) + rh * D + col;
-#pragma unroll
-    for (int e = 0; e < EL; e += 4) *reinterpret_cast<f32x4*>(dst + e) = f32x4{acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
-  } else {
-    __bf16* const dst = static_cast<__bf16*>(p.out) + rh * D + col;
-#pragma unroll
-    for (int e = 0; e < EL; e += 4)
-      *reinterpret_cast<bf16x4*>(dst + e) = bf16x4{static_cast<__bf16>(acc[e] * inv), static_cast<__bf16>(acc[e + 1] * inv), static_cast<__bf16>(acc[e + 2] * inv), static_cast<__bf16>(acc[e + 3] * inv)};
-  }
-  if (col == 0) p.lse[rh] = none ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
-}
-
 typedef int i32x2v __attribute__((ext_vector_type(2)));
 typedef i32x2v __attribute__((address_space(3))) * lds_i32x2_ptr;
 
@@ -87,72 +67,34 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
   const float c = p.scale_log2e;
   unsigned char* const ring = smem + w * NS * C::STAGE;
 
-  // ---- this workgroup's run of the call's work
-  PagedChunk<BM, BT> chunk;
-  const int64_t share = share_of<BM, BT>(p, chunk, lane);
-  int64_t at = share * blockIdx.x, left = share;
-  int seq = 64;                  // in the chunk
-  while (true) {
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(chunk.upto > at);
-    if (behind != 0) {
-      seq = __builtin_ctzll(behind);
-      at -= chunk.before(seq);
-      break;
-    }
-    at -= chunk.total();
-    if (chunk.base + 64 >= p.c.n_seqs) return;
-    chunk.load(p, chunk.base + 64, lane);
-  }
-  int n = 0, kv = 0, r0 = 0, row_tiles = 0, kt = 1, b = 0;
-  auto take = [&]() {
-    n = __builtin_amdgcn_readlane(chunk.s.n, seq);
-    kv = __builtin_amdgcn_readlane(chunk.s.kv, seq);
-    r0 = __builtin_amdgcn_readlane(chunk.s.r0, seq);
-    row_tiles = __builtin_amdgcn_readlane(chunk.row_tiles, seq);
-    kt = __builtin_amdgcn_readlane(chunk.key_tiles, seq);
-    b = chunk.base + seq;
-  };
-  take();
-  int unit = __builtin_amdgcn_readfirstlane(static_cast<int>(at / kt));
-  int from = __builtin_amdgcn_readfirstlane(static_cast<int>(at - static_cast<int64_t>(unit) * kt));
-
+  PagedRun<BM, BT> run;
+  const int worker = xcd_contiguous(blockIdx.x, p.workers);
+  if (!run.start(p, worker, lane)) return;
   const int64_t page_rows = static_cast<int64_t>(1) << p.c.ps_log2;
   const int ps_mask = static_cast<int>(page_rows) - 1;
-  while (left > 0) {
-    if (unit >= row_tiles * p.c.Hkv) {
-      unit = 0;
-      if (++seq == 64) {
-        if (chunk.base + 64 >= p.c.n_seqs) return;
-        chunk.load(p, chunk.base + 64, lane);
-        seq = 0;
-      }
-      if (chunk.base + seq >= p.c.n_seqs) return;
-      take();
-      continue;
-    }
-    const int upto = static_cast<int>(min(static_cast<int64_t>(kt), from + left));
-    const int head = unit / row_tiles, rt = unit - head * row_tiles;
-    const bool whole = from == 0 && upto == kt;
+  for (; run.next(p, lane); run.step()) {
+    const PagedSeq& s = run.s;
+    const int b = run.b, head = run.head, rt = run.rt;
+    const bool whole = run.whole();
 
     // ---- the rows
-    const int rows = n * p.G, m = rt * BM + lq, mc = min(m, rows - 1), tok = divide(mc, p.by_group);
+    const int rows = s.n * p.G, m = rt * BM + lq, mc = min(m, rows - 1), tok = divide(mc, p.by_group);
     const int tok0 = divide(rt * BM, p.by_group), tok1 = divide(min(rt * BM + BM, rows) - 1, p.by_group);
-    const PagedSeq s{n, kv, r0};
     const PagedKeys keys = keys_of<BM, BT>(p, s, tok0, tok1);
-    const int p0 = kv - n;
+    const int p0 = s.kv - s.n;
     const int see_to = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1);         // the lane's row sees keys up to it,
     const int see_from = p.window > 0 ? p0 + tok - p.window + 1 : INT_MIN;       // from this one on or among the first
     const int all_to = min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1), all_from = p.window > 0 ? p0 + tok1 - p.window + 1 : INT_MIN;
     bf16x8 qf[D / 32];
     {
-      const __bf16* const src = static_cast<const __bf16*>(p.q) + static_cast<int64_t>(r0 + tok) * p.q_stride + static_cast<int64_t>(head * p.G + mc - tok * p.G) * D;
+      const __bf16* const src = static_cast<const __bf16*>(p.q) + static_cast<int64_t>(s.r0 + tok) * p.q_stride + static_cast<int64_t>(head * p.G + mc - tok * p.G) * D;
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) qf[j] = *reinterpret_cast<const bf16x8*>(src + (F8 ? 64 * (j / 2) + 16 * g + 8 * (j % 2) : 32 * j + 8 * g));
     }
     f32x4 o[NDB];
     float m_run, l_run, l_lo;
 
-    const int t0 = min(from, keys.n_tiles), t1 = min(upto, keys.n_tiles);
+    const int t0 = key_tile_at(run.x0, run.cost, keys.n_tiles), t1 = key_tile_at(run.x1, run.cost, keys.n_tiles);
     // ---- pages of the wavefront's keys, LIST / 2 tiles at a time
     int listed = t0;
     auto look_up = [&](int t) {
@@ -391,87 +333,42 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
     for (int i = 0; i < NW; ++i)
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] += weight[i] * sums[(i * BM + jr) * C::ROW + je + e];
+    const float inv = total == 0.f ? 0.f : 1.f / total, lse2 = total == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(total);
+#pragma unroll
+    for (int e = 0; e < EL; ++e) acc[e] *= inv;
     if (rt * BM + jr < rows) {
       if (whole) {
         const int jt = divide(rt * BM + jr, p.by_group);
-        finish_row<D, EL>(p, (static_cast<int64_t>(r0 + jt)) * p.Hq + head * p.G + (rt * BM + jr - jt * p.G), je, acc, top, total);
+        store_row<D, EL>(p, static_cast<int64_t>(s.r0 + jt) * p.Hq + head * p.G + (rt * BM + jr - jt * p.G), je, acc, lse2);
       } else {
-        float* const dst = p.part + (2 * static_cast<int64_t>(blockIdx.x) + (from == 0 ? 1 : 0)) * part_floats(BM, D);
+        float* const dst = part_of<BM, D>(p, worker, run.x0 > 0);
 #pragma unroll
-        for (int e = 0; e < EL; ++e) dst[jr * D + je + e] = acc[e];
-        if (je == 0) { dst[BM * D + jr] = top; dst[BM * D + BM + jr] = total; }
+        for (int e = 0; e < EL; e += 4) *reinterpret_cast<f32x4*>(dst + jr * D + je + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+        if (je == 0) dst[BM * D + jr] = lse2;
       }
     }
     __syncthreads();
-    left -= upto - from;
-    from = 0;
-    ++unit;
   }
-}
-
-// A row tile whose keys several workgroups took: its partial results, in their order.
-template <int D, bool F8>
-__global__ __launch_bounds__(256) void paged_rows_combine(const PagedAttn p) {
-  using C = RowsCfg<D, F8>;
-  constexpr int BM = C::BM, BT = C::BT, EL = D / 16;
-  const int thread = threadIdx.x, lane = thread & 63;
-  PagedChunk<BM, BT> chunk;
-  const int64_t share = share_of<BM, BT>(p, chunk, lane);
-  int64_t unit = blockIdx.x, start = 0;
-  int seq;
-  while (true) {
-    const int64_t units = static_cast<int64_t>(chunk.row_tiles) * p.c.Hkv, upto = wave_prefix(units, lane);
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(upto > unit);
-    if (behind != 0) {
-      seq = __builtin_ctzll(behind);
-      if (seq > 0) unit -= __shfl(upto, seq - 1);
-      start += chunk.before(seq);
-      break;
-    }
-    unit -= __shfl(upto, 63);
-    start += chunk.total();
-    if (chunk.base + 64 >= p.c.n_seqs) return;
-    chunk.load(p, chunk.base + 64, lane);
-  }
-  const int kt = __shfl(chunk.key_tiles, seq), row_tiles = __shfl(chunk.row_tiles, seq), rows = __shfl(chunk.s.n, seq) * p.G, r0 = __shfl(chunk.s.r0, seq);
-  start += unit * kt;
-  const int64_t first = start / share, last = (start + kt - 1) / share;
-  if (first == last) return;
-  const int head = static_cast<int>(unit) / row_tiles, rt = static_cast<int>(unit) - head * row_tiles;
-  const int jr = thread / 16, je = thread % 16 * EL;
-  if (rt * BM + jr >= rows) return;
-  float top = kNegBig, total = 0.f, acc[EL];
-#pragma unroll
-  for (int e = 0; e < EL; ++e) acc[e] = 0.f;
-  for (int64_t i = first; i <= last; ++i) {
-    const float* const src = p.part + (2 * i + (i == first ? 1 : 0)) * part_floats(BM, D);
-    const float m = src[BM * D + jr], m_new = fmaxf(top, m), a = fast_exp2(top - m_new), b = fast_exp2(m - m_new);
-    total = total * a + src[BM * D + BM + jr] * b;
-#pragma unroll
-    for (int e = 0; e < EL; ++e) acc[e] = acc[e] * a + src[jr * D + je + e] * b;
-    top = m_new;
-  }
-  const int jt = divide(rt * BM + jr, p.by_group);
-  finish_row<D, EL>(p, static_cast<int64_t>(r0 + jt) * p.Hq + head * p.G + (rt * BM + jr - jt * p.G), je, acc, top, total);
 }
 
 template <int D, bool F8>
 hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
   using C = RowsCfg<D, F8>;
-  const int64_t units = (static_cast<int64_t>(p.c.n_rows) * p.G / C::BM + p.c.n_seqs) * p.c.Hkv;
-  if (units > INT_MAX) return hipErrorInvalidValue;
   const hipError_t e = TASP_LAUNCH((paged_rows_kernel<D, F8>), dim3(static_cast<unsigned>(p.workers)), dim3(C::NW * 64), stream, p);
-  if (e != hipSuccess) return e;
-  return TASP_LAUNCH((paged_rows_combine<D, F8>), dim3(static_cast<unsigned>(units)), dim3(256), stream, p);
+  return e != hipSuccess ? e : launch_paged_combine<D, C::BM, C::BT>(p, stream);
 }
+
+constexpr int kWorkers = 512;
 
 }  // namespace
 
-int paged_rows_workers(bool, int) { return 512; }
-int64_t paged_rows_workspace(bool e4m3, int d) { return 2 * static_cast<int64_t>(paged_rows_workers(e4m3, d)) * part_floats(16, d) * 4; }
+int64_t paged_rows_workspace(int d) { return 2 * kWorkers * part_floats(16, d) * 4; }
 
 hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
-  p.workers = paged_rows_workers(e4m3, d);
+  p.workers = kWorkers;
+  p.tile_cost = kParts / 4;
+  p.snap = kParts / 4;
+  p.least_share = kParts;
   if (d == 64) return e4m3 ? launch_variant<64, true>(p, stream) : launch_variant<64, false>(p, stream);
   return e4m3 ? launch_variant<128, true>(p, stream) : launch_variant<128, false>(p, stream);
 }

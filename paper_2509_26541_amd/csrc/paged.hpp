@@ -66,7 +66,8 @@ struct PagedAttn {
   int64_t q_stride;              // elements between the tokens of q
   int32_t Hq, G, causal, window, sinks, out_fp32;
   float scale_log2e;
-  int32_t workers;               // workgroups that share the keys
+  int32_t workers;               // workgroups that share the work, and how they do (in parts of a key tile, see PagedCost): what a row
+  int32_t tile_cost, snap, least_share;      // tile costs beside its keys, the least that is split off one, the least that a worker takes
   Divider by_group;
 };
 
@@ -90,22 +91,50 @@ __host__ __device__ __forceinline__ PagedKeys keys_of(const PagedAttn& p, const 
   return k;
 }
 
-// What a sequence costs, in key tiles: row tiles, and key tiles of each of them at most.  A row tile without keys counts as
-// one: its rows are written too.
+// What the rows of a sequence cost, in parts of a key tile: row tile i of a KV head costs first + i step.  Under the causal mask later
+// row tiles see more keys; with a window all are taken for as long as the longest.  Every row tile costs something: its rows are written.
+constexpr int kParts = 1024;
+struct PagedCost { int row_tiles; int64_t first, step; };
 template <int BM, int BT>
-__host__ __device__ __forceinline__ void cost_of(const PagedAttn& p, const PagedSeq& s, int& row_tiles, int& key_tiles) {
-  row_tiles = (s.n * p.G + BM - 1) / BM;
-  int t = (s.kv + BT - 1) / BT;
+__host__ __device__ __forceinline__ PagedCost cost_of(const PagedAttn& p, const PagedSeq& s) {
+  PagedCost c{(s.n * p.G + BM - 1) / BM, 0, 0};
+  int64_t keys = p.causal ? larger(s.kv - s.n, 0) + lesser(s.n, BM / p.G + 1) : s.kv;
+  if (p.causal) c.step = static_cast<int64_t>(kParts) * BM / BT / p.G;
   if (p.window > 0) {
-    const int64_t w = (static_cast<int64_t>(lesser(p.sinks, s.kv)) + BT - 1) / BT + (static_cast<int64_t>(p.window) + BM / p.G + 1 + BT - 1) / BT + 1;
-    t = static_cast<int>(lesser(static_cast<int64_t>(t), w));
+    const int64_t most = static_cast<int64_t>(p.window) + BM / p.G + BT + lesser(p.sinks, s.kv);
+    if (keys + static_cast<int64_t>(c.row_tiles) * BM / p.G > most) {
+      keys = lesser<int64_t>(s.kv, most);
+      c.step = 0;
+    }
   }
-  key_tiles = larger(1, t);
+  c.first = keys * (kParts / BT) + p.tile_cost;
+  return c;
+}
+// All of the first n row tiles.
+__host__ __device__ __forceinline__ int64_t cost_upto(const PagedCost& c, int64_t n) { return n * c.first + c.step * (n * (n - 1) / 2); }
+// The row tile that x parts into a KV head's work fall in (0 <= x < cost_upto(c, row_tiles)).
+__host__ __device__ __forceinline__ int row_tile_at(const PagedCost& c, int64_t x) {
+  const float b = static_cast<float>(c.first) - 0.5f * static_cast<float>(c.step), s = static_cast<float>(c.step);
+  const float guess = c.step == 0 ? static_cast<float>(x) / b : 2.f * static_cast<float>(x) / (b + sqrtf(b * b + 2.f * s * static_cast<float>(x)));
+  int i = lesser(larger(static_cast<int>(guess), 0), c.row_tiles - 1);
+  while (i > 0 && cost_upto(c, i) > x) --i;
+  while (i + 1 < c.row_tiles && cost_upto(c, i + 1) <= x) ++i;
+  return i;
+}
+// A run that starts or ends x parts into a row tile of cost `cost` does so at a key tile; one that would leave less than `snap` on a side
+// takes or leaves the row tile as a whole.
+__host__ __device__ __forceinline__ int64_t snapped(int64_t x, int64_t cost, int64_t snap) { return x < snap ? 0 : cost - x < snap ? cost : x; }
+__host__ __device__ __forceinline__ int key_tile_at(int64_t x, int64_t cost, int n_tiles) {
+  return x >= cost ? n_tiles : static_cast<int>(x * n_tiles / cost);
 }
 
 // A value that all lanes have, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32));
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), lane);
   return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
@@ -118,27 +147,22 @@ __device__ __forceinline__ int64_t wave_prefix(int64_t x, int lane) {
   return x;
 }
 
-// 64 sequences, one to a lane, with their work laid end to end: sequence after sequence, KV head after KV head, row tile after row
-// tile, each `key_tiles` long.
+// 64 sequences, one to a lane, with their work laid end to end: sequence after sequence, KV head after KV head, row tile after row tile.
 template <int BM, int BT>
 struct PagedChunk {
   int base;
   PagedSeq s;
-  int row_tiles, key_tiles;
-  int64_t len, upto;             // of the lane's sequence; with all before it in this chunk
+  PagedCost c;
+  int64_t head, upto;            // work of a KV head; of this sequence and all before it in this chunk
   __device__ __forceinline__ void load(const PagedAttn& p, int first, int lane) {
     base = first;
     s = load_seq(p.c, first + lane);
-    cost_of<BM, BT>(p, s, row_tiles, key_tiles);
-    len = static_cast<int64_t>(row_tiles) * p.c.Hkv * key_tiles;
-    upto = wave_prefix(len, lane);
+    c = cost_of<BM, BT>(p, s);
+    head = cost_upto(c, c.row_tiles);
+    upto = wave_prefix(head * p.c.Hkv, lane);
   }
-  __device__ __forceinline__ int64_t total() const { return before(64); }
   // work of the chunk's first `i` sequences
-  __device__ __forceinline__ int64_t before(int i) const {
-    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(upto), i - 1), hi = __builtin_amdgcn_readlane(static_cast<int>(upto >> 32), i - 1);
-    return i == 0 ? 0 : static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-  }
+  __device__ __forceinline__ int64_t before(int i) const { return i == 0 ? 0 : of_lane(upto, i - 1); }
 };
 
 // All work of a call, and how much of it a worker takes.
@@ -147,21 +171,112 @@ __device__ __forceinline__ int64_t share_of(const PagedAttn& p, PagedChunk<BM, B
   int64_t all = 0;
   for (int first = 0; first < p.c.n_seqs; first += 64) {
     c.load(p, first, lane);
-    all += c.total();
+    all += c.before(64);
   }
   if (c.base != 0) c.load(p, 0, lane);
-  return uniform((all + p.workers - 1) / p.workers);
+  return larger<int64_t>((all + p.workers - 1) / p.workers, p.least_share);
 }
 
-// Floats of a partial result: BM rows of d sums, their running maxima and their sums of weights.
-constexpr int64_t part_floats(int bm, int d) { return static_cast<int64_t>(bm) * (d + 2); }
+// A worker's run of the call's work, one row tile (or piece of one) after the other.
+template <int BM, int BT>
+struct PagedRun {
+  PagedChunk<BM, BT> chunk;
+  int64_t share, from, to;       // the run, in parts from the start of sequence `seq` of the chunk
+  int seq, head, rt;             // the next row tile
+  PagedSeq s;
+  PagedCost c;
+  int64_t at, cost;              // where it starts, and its cost
+  int64_t x0, x1;                // what the run has of it
+  int b;
 
-// Implemented in cache.hip and attn_paged.hip.
+  __device__ __forceinline__ void take() {
+    s.n = __builtin_amdgcn_readlane(chunk.s.n, seq);
+    s.kv = __builtin_amdgcn_readlane(chunk.s.kv, seq);
+    s.r0 = __builtin_amdgcn_readlane(chunk.s.r0, seq);
+    c.row_tiles = __builtin_amdgcn_readlane(chunk.c.row_tiles, seq);
+    c.first = of_lane(chunk.c.first, seq);
+    c.step = of_lane(chunk.c.step, seq);
+    b = chunk.base + seq;
+  }
+  // false: no work for this worker
+  __device__ __forceinline__ bool start(const PagedAttn& p, int worker, int lane) {
+    share = share_of<BM, BT>(p, chunk, lane);
+    from = share * worker;
+    to = from + share;
+    while (true) {
+      const uint64_t behind = __builtin_amdgcn_ballot_w64(chunk.upto > from);
+      if (behind != 0) {
+        seq = __builtin_ctzll(behind);
+        const int64_t before = chunk.before(seq);
+        from -= before;
+        to -= before;
+        break;
+      }
+      const int64_t before = chunk.before(64);
+      from -= before;
+      to -= before;
+      if (chunk.base + 64 >= p.c.n_seqs) return false;
+      chunk.load(p, chunk.base + 64, lane);
+    }
+    take();
+    const int64_t one = cost_upto(c, c.row_tiles);
+    head = static_cast<int>(from / one);
+    rt = row_tile_at(c, from - head * one);
+    at = head * one + cost_upto(c, rt);
+    return true;
+  }
+  // false: the run is over
+  __device__ __forceinline__ bool next(const PagedAttn& p, int lane) {
+    while (at < to) {
+      if (rt >= c.row_tiles) {
+        rt = 0;
+        ++head;
+      }
+      if (head >= p.c.Hkv || c.row_tiles == 0) {
+        head = rt = 0;
+        from -= at;
+        to -= at;
+        at = 0;
+        if (++seq == 64) {
+          if (chunk.base + 64 >= p.c.n_seqs) return false;
+          chunk.load(p, chunk.base + 64, lane);
+          seq = 0;
+        }
+        if (chunk.base + seq >= p.c.n_seqs) return false;
+        take();
+        continue;
+      }
+      cost = c.first + rt * c.step;
+      x0 = snapped(larger<int64_t>(from - at, 0), cost, p.snap);
+      x1 = to - at >= cost ? cost : snapped(to - at, cost, p.snap);
+      if (x0 < x1) return true;
+      step();
+    }
+    return false;
+  }
+  __device__ __forceinline__ void step() {
+    at += cost;
+    ++rt;
+  }
+  __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == cost; }
+};
+
+// A partial result: BM rows of d normalised sums, and their log-sum-exps to base 2.  A worker leaves at most two: of the row tile that its run
+// starts in, and of the one that it ends in.
+constexpr int64_t part_floats(int bm, int d) { return static_cast<int64_t>(bm) * (d + 1); }
+template <int BM, int D>
+__device__ __forceinline__ float* part_of(const PagedAttn& p, int64_t worker, bool starts_inside) {
+  return p.part + (2 * worker + (starts_inside ? 0 : 1)) * part_floats(BM, D);
+}
+
+// Implemented in cache.hip.
 hipError_t launch_cache_write(const PagedView& c, bool e4m3, const void* k, const void* v, int64_t k_stride, int64_t v_stride, bool fp32, int d, hipStream_t stream);
 hipError_t launch_cache_read(const PagedView& c, bool e4m3, void* k, void* v, bool fp32, int d, hipStream_t stream);
-// workgroups that launch_paged_rows deals a call's keys to, and the bytes of their partial results
-int paged_rows_workers(bool e4m3, int d);
-int64_t paged_rows_workspace(bool e4m3, int d);
+// Implemented in attn_paged.hip and attn_paged_tile.hip: the kernels for up to 16 rows (token, query head of the group) to a sequence and KV
+// head, and for more; and the bytes of workspace that each takes.
 hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, hipStream_t stream);
+int64_t paged_rows_workspace(int d);
+hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream);
+int64_t paged_tile_workspace(int d);
 
 }  // namespace tasp

@@ -79,6 +79,7 @@ def _check(out, lse, want, d, fp32=False):
 BATCHES = {
     "one": ([1], [1]), "few": ([1, 1, 1], [17, 130, 33]), "edges": ([1, 2, 1, 3, 1, 1], [15, 16, 31, 64, 127, 129]),
     "empty": ([0, 1, 0, 2, 0], [5, 0, 0, 40, 9]), "short": ([5, 1], [2, 1]), "chunk": ([37, 1, 50], [37, 200, 131]), "long": ([2, 1], [1500, 2111]),
+    "prompt": ([200, 129, 1], [200, 700, 77]), "tiles": ([64, 65, 63, 33], [64, 129, 1023, 1025]),
     "many": ([1] * 70 + [3], [3 * i % 97 for i in range(70)] + [301]),
 }
 HEADS = [(4, 4, 128), (8, 2, 64), (6, 2, 128), (16, 1, 64), (5, 5, 64), (24, 1, 128)]

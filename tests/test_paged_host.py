@@ -165,13 +165,15 @@ static void tiles(const PagedAttn& p, const std::vector<int>& seen) {
   for (int b = 0; b < p.c.n_seqs; ++b) {
     const PagedSeq s = load_seq(p.c, b);
     expect(s.r0 >= 0 && s.n >= 0 && s.r0 + s.n <= p.c.n_rows && s.kv >= 0 && s.kv <= p.c.cap, "sequence");
-    int row_tiles, key_tiles;
-    cost_of<BM, BT>(p, s, row_tiles, key_tiles);
-    expect(key_tiles >= 1 && static_cast<int64_t>(row_tiles) * BM >= static_cast<int64_t>(s.n) * p.G, "cost");
+    const PagedCost c = cost_of<BM, BT>(p, s);
+    const int row_tiles = c.row_tiles;
+    expect(static_cast<int64_t>(row_tiles) * BM >= static_cast<int64_t>(s.n) * p.G && c.first > 0 && c.step >= 0, "cost");
+    for (int i = 0; i < row_tiles; ++i)
+      for (int64_t x : {cost_upto(c, i), cost_upto(c, i) + 1, cost_upto(c, i + 1) - 1}) expect(row_tile_at(c, x) == i, "row tile");
     for (int rt = 0; rt < row_tiles; ++rt) {
       const int rows = s.n * p.G, tok0 = rt * BM / p.G, tok1 = (lesser(rt * BM + BM, rows) - 1) / p.G;
       const PagedKeys k = keys_of<BM, BT>(p, s, tok0, tok1);
-      expect(k.end >= 0 && k.end <= p.c.cap && k.n_tiles >= 0 && k.n_tiles <= key_tiles, "tiles");
+      expect(k.end >= 0 && k.end <= p.c.cap && k.n_tiles >= 0, "tiles");
       // every visible key of every row is in a tile, and no tile comes twice
       int last = -1;
       for (int u = 0; u < k.n_tiles; ++u) { expect(k.tile(u) > last && k.tile(u) * BT < k.end, "order"); last = k.tile(u); }
@@ -196,6 +198,38 @@ static void tiles(const PagedAttn& p, const std::vector<int>& seen) {
     }
   }
 }
+// The runs of all workers: every key tile of every row tile is taken once, by the workers that the sum of the parts goes by.
+template <int BM, int BT>
+static void runs(const PagedAttn& p) {
+  int64_t all = 0;
+  for (int b = 0; b < p.c.n_seqs; ++b) { const PagedCost c = cost_of<BM, BT>(p, load_seq(p.c, b)); all += cost_upto(c, c.row_tiles) * p.c.Hkv; }
+  const int64_t share = larger<int64_t>((all + p.workers - 1) / p.workers, p.least_share);
+  int64_t start = 0;
+  for (int b = 0; b < p.c.n_seqs; ++b) {
+    const PagedSeq s = load_seq(p.c, b);
+    const PagedCost c = cost_of<BM, BT>(p, s);
+    for (int i = 0; i < c.row_tiles * p.c.Hkv; ++i) {
+      const int64_t cost = c.first + i % c.row_tiles * c.step;
+      const int tiles = rnd() % 50;
+      const int64_t first = (start + p.snap + share - 1) / share - 1, last = (start + cost - p.snap) / share;
+      const bool parts = cost >= 2 * p.snap && first < last;
+      int upto = 0, takers = 0;
+      for (int64_t w = larger<int64_t>(start / share - 1, 0); w <= (start + cost) / share; ++w) {
+        const int64_t from = w * share, to = from + share;
+        if (to <= start || from >= start + cost) continue;
+        const int64_t x0 = snapped(larger<int64_t>(from - start, 0), cost, p.snap), x1 = to - start >= cost ? cost : snapped(to - start, cost, p.snap);
+        if (x0 >= x1) continue;
+        expect(w < p.workers, "worker");
+        expect(parts ? w >= first && w <= last && (x0 == 0) == (w == first) : x0 == 0 && x1 == cost, "part");
+        expect(key_tile_at(x0, cost, tiles) == upto, "gap");
+        upto = key_tile_at(x1, cost, tiles);
+        ++takers;
+      }
+      expect(upto == tiles && takers == (parts ? last - first + 1 : 1), "row tile not taken whole");
+      start += cost;
+    }
+  }
+}
 int main() {
   for (int round = 0; round < 400; ++round) {
     const bool wild = round % 2 == 0;
@@ -207,8 +241,10 @@ int main() {
     PagedAttn p{};
     p.c.table = table.data(); p.c.kv_len = kv.data(); p.c.row_start = start.data();
     p.c.n_pages = 7; p.c.ps_log2 = ps_log2; p.c.Hkv = 2; p.c.n_seqs = n_seqs; p.c.max_pages = max_pages; p.c.n_rows = n_rows; p.c.cap = max_pages << ps_log2;
-    p.G = 1 + rnd() % 9; p.causal = rnd() % 4 != 0; p.window = p.causal && rnd() % 2 ? 1 + rnd() % 100 : 0; p.sinks = p.window ? rnd() % 70 : 0;
+    p.G = 1 + rnd() % 9; p.tile_cost = 1; p.causal = rnd() % 4 != 0; p.window = p.causal && rnd() % 2 ? 1 + rnd() % 100 : 0; p.sinks = p.window ? rnd() % 70 : 0;
     if (p.window && rnd() % 5 == 0) { p.window = 1 << 30; p.sinks = 2147483647; }
+    p.workers = 1 + rnd() % 300; p.tile_cost = rnd() % 3000; p.snap = 1 + rnd() % 5000; p.least_share = 1 + rnd() % 9000;
+    if (!wild) { runs<16, 128>(p); runs<128, 64>(p); runs<16, 64>(p); }
     tiles<16, 64>(p, table);
     tiles<16, 128>(p, table);
     tiles<128, 64>(p, table);
