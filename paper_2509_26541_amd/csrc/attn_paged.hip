@@ -53,6 +53,8 @@ __device__ __forceinline__ bf16x8 widen(u32x2 w) {
   return r.v;
 }
 
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 typedef int i32x2v __attribute__((ext_vector_type(2)));
 typedef i32x2v __attribute__((address_space(3))) * lds_i32x2_ptr;
 
@@ -70,17 +72,17 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
   PagedRun<BM, BT> run;
   const int worker = xcd_contiguous(blockIdx.x, p.workers);
   if (!run.start(p, worker, lane)) return;
-  const int64_t page_rows = static_cast<int64_t>(1) << p.c.ps_log2;
-  const int ps_mask = static_cast<int>(page_rows) - 1;
+  const unsigned page_bytes = (static_cast<unsigned>(p.c.Hkv) << p.c.ps_log2) * RB;            // (below 2^31, the host sees to it)
+  const int ps_mask = (1 << p.c.ps_log2) - 1;
   for (; run.next(p, lane); run.step()) {
     const PagedSeq& s = run.s;
-    const int b = run.b, head = run.head, rt = run.rt;
+    const int b = run.b, head = scalar(run.head), rt = scalar(run.rt);
     const bool whole = run.whole();
 
     // ---- the rows
     const int rows = s.n * p.G, m = rt * BM + lq, mc = min(m, rows - 1), tok = divide(mc, p.by_group);
     const int tok0 = divide(rt * BM, p.by_group), tok1 = divide(min(rt * BM + BM, rows) - 1, p.by_group);
-    const PagedKeys keys = keys_of<BM, BT>(p, s, tok0, tok1);
+    PagedKeys keys = keys_of<BM, BT>(p, s, tok0, tok1);
     const int p0 = s.kv - s.n;
     const int see_to = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1);         // the lane's row sees keys up to it,
     const int see_from = p.window > 0 ? p0 + tok - p.window + 1 : INT_MIN;       // from this one on or among the first
@@ -94,7 +96,14 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
     f32x4 o[NDB];
     float m_run, l_run, l_lo;
 
-    const int t0 = key_tile_at(run.x0, run.cost, keys.n_tiles), t1 = key_tile_at(run.x1, run.cost, keys.n_tiles);
+    // (what the loads and the loop go by is the same in all lanes, and said to be)
+    const int t0 = scalar(key_tile_at(run.x0, run.cost, keys.n_tiles)), t1 = scalar(key_tile_at(run.x1, run.cost, keys.n_tiles));
+    keys.n_first = scalar(keys.n_first);
+    keys.from = scalar(keys.from);
+    keys.end = scalar(keys.end);
+    const int64_t head_bytes = (static_cast<int64_t>(head) << p.c.ps_log2) * RB;
+    const unsigned char* const k_head = p.c.k + head_bytes;
+    const unsigned char* const v_head = p.c.v + head_bytes;
     // ---- pages of the wavefront's keys, LIST / 2 tiles at a time
     int listed = t0;
     auto look_up = [&](int t) {
@@ -111,35 +120,38 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
+    auto listed_pages = [&](int u) {
+      if (u - listed >= C::LIST / 2) look_up(u);
+      return *reinterpret_cast<const i32x2v*>(&pages[w][(u - listed) * 2]);
+    };
     // K and V of the wavefront's 32 keys of tile u into stage st; keys behind the end and keys without a page come as zeros.
     // `paged` takes two bits a tile: whether each 16 keys have a page.
     unsigned paged = 0;
-    auto fetch = [&](int u, int st) {
-      if (u - listed >= C::LIST / 2) look_up(u);
-      const int e = (u - listed) * 2;
-      const int page0 = __builtin_amdgcn_readfirstlane(pages[w][e]), page1 = __builtin_amdgcn_readfirstlane(pages[w][e + 1]);
+    auto fetch = [&](int u, int st, i32x2v listed_at) {
+      const int page[2] = {__builtin_amdgcn_readfirstlane(listed_at[0]), __builtin_amdgcn_readfirstlane(listed_at[1])};
       const int pos0 = keys.tile(u) * BT + w * C::WK;
       unsigned char* const dst = ring + st * C::STAGE;
-      paged = paged << 2 | (page0 >= 0 ? 1u : 0u) | (page1 >= 0 ? 2u : 0u);
+      paged = paged << 2 | (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int page = i == 0 ? page0 : page1, pos = pos0 + 16 * i, slot = pos & ps_mask;
-        const int64_t base = ((static_cast<int64_t>(max(page, 0)) * p.c.Hkv + head) << p.c.ps_log2) * RB;
-        const unsigned records = page < 0 ? 0u : static_cast<unsigned>(max(0, min(static_cast<int>(page_rows), keys.end - pos + slot))) * RB;
-        const u32x4 kb = raw_buffer(p.c.k + base, records), vb = raw_buffer(p.c.v + base, records);
+        const int pos = pos0 + 16 * i;
+        const int64_t base = static_cast<int64_t>(static_cast<uint64_t>(static_cast<unsigned>(max(page[i], 0))) * page_bytes) + static_cast<unsigned>((pos & ps_mask) * RB);
+        const int n = max(0, scalar(min(16, keys.end - pos)));       // (both bounds at once would be a vector instruction)
+        const unsigned records = page[i] < 0 ? 0u : static_cast<unsigned>(n) * RB;
+        const u32x4 kb = raw_buffer(k_head + base, records), vb = raw_buffer(v_head + base, records);
 #pragma unroll
         for (int j = 0; j < C::LOADS / 2; ++j) {
           const int r = 16 * i + j * C::RPL + lane / C::UNITS;       // of the stage's 32
-          const unsigned soff = min(static_cast<unsigned>((slot + j * C::RPL) * RB), records);
+          const unsigned soff = min(static_cast<unsigned>(j * C::RPL * RB), records);
           const unsigned row = static_cast<unsigned>(lane / C::UNITS * RB), un = lane % C::UNITS;
-          buffer_to_lds_16<true>(kb, soff, row + (un ^ C::swz_k(r)) * 16, dst + (16 * i + j * C::RPL) * RB);
-          buffer_to_lds_16<true>(vb, soff, row + (un ^ C::swz_v(r)) * 16, dst + (C::WK + 16 * i + j * C::RPL) * RB);
+          buffer_to_lds_16_once(kb, soff, row + (un ^ C::swz_k(r)) * 16, dst + (16 * i + j * C::RPL) * RB);
+          buffer_to_lds_16_once(vb, soff, row + (un ^ C::swz_v(r)) * 16, dst + (C::WK + 16 * i + j * C::RPL) * RB);
         }
       }
       if constexpr (F8) {
         // the scales: 16 bytes for each 16 keys of K, then of V
-        const int i = lane / 4 % 2, page = max(i == 0 ? page0 : page1, 0), slot = (pos0 + 16 * i) & ps_mask;
-        const unsigned char* const sc = (lane / 8 % 2 == 0 ? p.c.k_scale : p.c.v_scale) + ((static_cast<int64_t>(page) * p.c.Hkv + head) << p.c.ps_log2) + slot + lane % 4 * 4;
+        const int pg = max(lane & 4 ? page[1] : page[0], 0), slot = (pos0 + (lane & 4) * 4) & ps_mask;
+        const unsigned char* const sc = (lane & 8 ? p.c.v_scale : p.c.k_scale) + ((static_cast<int64_t>(pg) * p.c.Hkv + head) << p.c.ps_log2) + slot + lane % 4 * 4;
         const unsigned to = static_cast<unsigned>(reinterpret_cast<size_t>((lds_void_ptr)(dst + 2 * C::WK * RB)));
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(to), "v"(sc) : "memory");
       }
@@ -148,7 +160,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
     // Zero times an infinity or a NaN would carry V's values to rows that do not see them, and what rounding left of a probability,
     // times an infinity, is NaN for those that do.  Sums that are not finite are formed again, with the rows of V that hold
     // such values taken out of the product and added one by one.
-    for (int careful = 0;; ++careful) {
+    auto pass = [&](auto careful) {
 #pragma unroll
       for (int i = 0; i < NDB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       m_run = kNegBig; l_run = 0.f; l_lo = 0.f;
@@ -157,9 +169,10 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
         look_up(t0);
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) asm volatile("" : "+v"(qf[j]));          // (the compiler waits for them here, not in the loop)
-        for (int i = 0; i < NS; ++i) fetch(t0 + i, i);
+        for (int i = 0; i < NS; ++i) fetch(t0 + i, i, listed_pages(t0 + i));
       }
       for (int t = t0, st = 0; t < t1; ++t, st = st + 1 == NS ? 0 : st + 1) {
+        const i32x2v soon = listed_pages(t + NS);
         asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NS - 1) * C::PER_STAGE) : "memory");
         const unsigned char* const kl = ring + st * C::STAGE;
         unsigned char* const vl = ring + st * C::STAGE + C::WK * RB;
@@ -234,12 +247,16 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
         l_lo += sum;
         if ((t & 63) == 63) { l_run += l_lo; l_lo = 0.f; }
 
-        if (careful != 0) {
+        if constexpr (decltype(careful)::value) {
+          // (places formed here: outside the loop they would take registers from it)
+          int ln = lane;
+          asm volatile("" : "+v"(ln));
+          const int cg = ln >> 4, cq = ln & 15;
           // rows of V with a value that is not finite: two lanes look at each
           bool odd = false;
 #pragma unroll
           for (int i = 0; i < RB / 32; ++i) {
-            const u32x4 y = *reinterpret_cast<const u32x4*>(vl + lane / 2 * RB + (lane % 2 * (RB / 32) + i) * 16);
+            const u32x4 y = *reinterpret_cast<const u32x4*>(vl + ln / 2 * RB + (ln % 2 * (RB / 32) + i) * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               if constexpr (F8) {
@@ -253,7 +270,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
           uint64_t rows_odd = __builtin_amdgcn_ballot_w64(odd);
           rows_odd = (rows_odd | rows_odd >> 1) & 0x5555555555555555ull;
           while (rows_odd != 0) {
-            const int r = __builtin_ctzll(rows_odd) / 2, at_e = r / 16 * 4 + r % 4, from_lane = r % 16 / 4 * 16 + lq;
+            const int r = __builtin_ctzll(rows_odd) / 2, at_e = r / 16 * 4 + r % 4, from_lane = r % 16 / 4 * 16 + cq;
             rows_odd &= rows_odd - 1;
             float pr = 0.f;
 #pragma unroll
@@ -264,10 +281,10 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
             for (int db = 0; db < NDB; ++db)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const int col = 16 * db + 4 * g + e;
+                const int col = 16 * db + 4 * cg + e;
                 float y;
                 if constexpr (F8) {
-                  const unsigned byte = vl[r * RB + (db ^ C::swz_v(r)) * 16 + 4 * g + e];
+                  const unsigned byte = vl[r * RB + (db ^ C::swz_v(r)) * 16 + 4 * cg + e];
                   y = __builtin_amdgcn_cvt_f32_fp8(byte, 0);
                 } else {
                   y = static_cast<float>(*reinterpret_cast<const __bf16*>(vl + r * RB + ((col / 8) ^ C::swz_v(r)) * 16 + col % 8 * 2));
@@ -275,7 +292,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
                 o[db][e] += sees ? pr * y : 0.f;
               }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (lane < C::UNITS) *reinterpret_cast<u32x4*>(vl + r * RB + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+            if (ln < C::UNITS) *reinterpret_cast<u32x4*>(vl + r * RB + ln * 16) = u32x4{0u, 0u, 0u, 0u};
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           }
         }
@@ -294,16 +311,18 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
           o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo, o[db], 0, 0, 0);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the stage has been read
-        fetch(t + NS, st);
+        fetch(t + NS, st, soon);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (what was fetched past the end lands in LDS too)
-      if (careful != 0) break;
+    };
+    pass(std::false_type{});
+    {
       float z = 0.f;
 #pragma unroll
       for (int i = 0; i < NDB; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[i][e], 0.f, z);
-      if (__builtin_amdgcn_ballot_w64(z != 0.f) == 0) break;     // (0 times a number is 0)
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(z != 0.f) != 0, 0)) pass(std::true_type{});       // (0 times a number is 0)
     }
 
     // ---- the wavefronts' sums are joined
@@ -366,6 +385,7 @@ int64_t paged_rows_workspace(int d) { return 2 * kWorkers * part_floats(16, d) *
 
 hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
   p.workers = kWorkers;
+  p.by_workers = 1.0 / p.workers;
   p.tile_cost = kParts / 4;
   p.snap = kParts / 4;
   p.least_share = kParts;

@@ -534,6 +534,7 @@ int64_t paged_tile_workspace(int d) { return 2 * workers_of(d) * part_floats(128
 
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
   p.workers = workers_of(d);
+  p.by_workers = 1.0 / p.workers;
   p.tile_cost = 2 * kParts;
   p.snap = 4 * kParts;
   p.least_share = 4 * kParts;

@@ -31,14 +31,18 @@ __device__ __forceinline__ PagedPlace place_of_row(const PagedView& c, int64_t r
   return b < 0 || b >= c.n_seqs || row >= c.n_rows ? PagedPlace{-1, 0} : place_of(c, b, row);
 }
 
+// Both sides are read and written once: no place in the caches is asked for.
+template <class T>
+__device__ __forceinline__ T once(const T* p) { return __builtin_nontemporal_load(p); }
+
 template <class T>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
   if constexpr (sizeof(T) == 4) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+    const f32x4 a = once(reinterpret_cast<const f32x4*>(p)), b = once(reinterpret_cast<const f32x4*>(p) + 1);
 #pragma unroll
     for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
   } else {
-    const bf16x8 a = *reinterpret_cast<const bf16x8*>(p);
+    const bf16x8 a = __builtin_bit_cast(bf16x8, once(reinterpret_cast<const u32x4*>(p)));
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(a[e]);
   }
@@ -118,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(const PagedView c,
     for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
     if (at.page < 0) continue;
     if constexpr (F8) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(pages + in_row * D + piece * 8);
+      const u32x2 w = once(reinterpret_cast<const u32x2*>(pages + in_row * D + piece * 8));
       const float scale = scale_value((s == 0 ? c.k_scale : c.v_scale)[in_row]);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {

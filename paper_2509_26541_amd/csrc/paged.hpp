@@ -66,6 +66,7 @@ struct PagedAttn {
   int64_t q_stride;              // elements between the tokens of q
   int32_t Hq, G, causal, window, sinks, out_fp32;
   float scale_log2e;
+  double by_workers;             // 1 / workers
   int32_t workers;               // workgroups that share the work, and how they do (in parts of a key tile, see PagedCost): what a row
   int32_t tile_cost, snap, least_share;      // tile costs beside its keys, the least that is split off one, the least that a worker takes
   Divider by_group;
@@ -110,6 +111,20 @@ __host__ __device__ __forceinline__ PagedCost cost_of(const PagedAttn& p, const 
   c.first = keys * (kParts / BT) + p.tile_cost;
   return c;
 }
+// About 1 / x, and a / b rounded down (0 <= a < 2^52, b > 0): the compiler's 64-bit division is some 150 dependent instructions.
+__host__ __device__ __forceinline__ double reciprocal(double x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_rcp(x);
+#else
+  return 1.0 / x;
+#endif
+}
+__host__ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  int64_t q = static_cast<int64_t>(static_cast<double>(a) * reciprocal(static_cast<double>(b)));
+  while (q * b > a) --q;
+  while (a - q * b >= b) ++q;
+  return q;
+}
 // All of the first n row tiles.
 __host__ __device__ __forceinline__ int64_t cost_upto(const PagedCost& c, int64_t n) { return n * c.first + c.step * (n * (n - 1) / 2); }
 // The row tile that x parts into a KV head's work fall in (0 <= x < cost_upto(c, row_tiles)).
@@ -125,7 +140,7 @@ __host__ __device__ __forceinline__ int row_tile_at(const PagedCost& c, int64_t 
 // takes or leaves the row tile as a whole.
 __host__ __device__ __forceinline__ int64_t snapped(int64_t x, int64_t cost, int64_t snap) { return x < snap ? 0 : cost - x < snap ? cost : x; }
 __host__ __device__ __forceinline__ int key_tile_at(int64_t x, int64_t cost, int n_tiles) {
-  return x >= cost ? n_tiles : static_cast<int>(x * n_tiles / cost);
+  return x >= cost ? n_tiles : lesser(static_cast<int>(static_cast<double>(x) * reciprocal(static_cast<double>(cost)) * n_tiles), n_tiles);
 }
 
 // A value that all lanes have, in scalar registers.
@@ -138,12 +153,20 @@ __device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
   return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-__device__ __forceinline__ int64_t wave_prefix(int64_t x, int lane) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int64_t y = __shfl_up(x, s);
-    x += lane >= s ? y : 0;
-  }
+// Sums of the lanes up to and with each: lanes of a row of 16 pass theirs on by 1, 2, 4 and 8, then each row's and each half's last lane its own.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t passed_on(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), CTRL, ROWS, 0xf, false);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ int64_t wave_prefix(int64_t x) {
+  x += passed_on<0x111, 0xf>(x);
+  x += passed_on<0x112, 0xf>(x);
+  x += passed_on<0x114, 0xf>(x);
+  x += passed_on<0x118, 0xf>(x);
+  x += passed_on<0x142, 0xa>(x);
+  x += passed_on<0x143, 0xc>(x);
   return x;
 }
 
@@ -159,7 +182,7 @@ struct PagedChunk {
     s = load_seq(p.c, first + lane);
     c = cost_of<BM, BT>(p, s);
     head = cost_upto(c, c.row_tiles);
-    upto = wave_prefix(head * p.c.Hkv, lane);
+    upto = wave_prefix(head * p.c.Hkv);
   }
   // work of the chunk's first `i` sequences
   __device__ __forceinline__ int64_t before(int i) const { return i == 0 ? 0 : of_lane(upto, i - 1); }
@@ -174,7 +197,7 @@ __device__ __forceinline__ int64_t share_of(const PagedAttn& p, PagedChunk<BM, B
     all += c.before(64);
   }
   if (c.base != 0) c.load(p, 0, lane);
-  return larger<int64_t>((all + p.workers - 1) / p.workers, p.least_share);
+  return uniform(larger<int64_t>(static_cast<int64_t>(static_cast<double>(all) * p.by_workers) + 1, p.least_share));
 }
 
 // A worker's run of the call's work, one row tile (or piece of one) after the other.
@@ -220,7 +243,7 @@ struct PagedRun {
     }
     take();
     const int64_t one = cost_upto(c, c.row_tiles);
-    head = static_cast<int>(from / one);
+    head = static_cast<int>(quotient(from, one));
     rt = row_tile_at(c, from - head * one);
     at = head * one + cost_upto(c, rt);
     return true;

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
   int64_t unit = blockIdx.x / PER, start = 0;
   int seq;
   while (true) {
-    const int64_t upto = wave_prefix(static_cast<int64_t>(chunk.c.row_tiles) * p.c.Hkv, lane);
+    const int64_t upto = wave_prefix(static_cast<int64_t>(chunk.c.row_tiles) * p.c.Hkv);
     const uint64_t behind = __builtin_amdgcn_ballot_w64(upto > unit);
     if (behind != 0) {
       seq = __builtin_ctzll(behind);
@@ -56,29 +56,46 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
   start += head * cost_upto(c, c.row_tiles) + cost_upto(c, rt);
   const int64_t cost = c.first + rt * c.step;
   // runs that end inside the row tile: those of workers first .. last - 1, ends snapped to neither side
-  const int64_t first = (start + p.snap + share - 1) / share - 1, last = (start + cost - p.snap) / share;
-  if (cost < 2 * p.snap || first >= last) return;
+  if (cost < 2 * p.snap) return;
+  const int64_t first = quotient(start + p.snap + share - 1, share) - 1, last = quotient(start + cost - p.snap, share);
+  if (first >= last) return;
   const int jr = blockIdx.x % PER * 16 + thread / 16, je = thread % 16 * EL, m = rt * BM + jr;
   if (m >= n * p.G) return;
   float top = -__builtin_inff(), total = 0.f, acc[EL];
 #pragma unroll
   for (int e = 0; e < EL; ++e) acc[e] = 0.f;
-  for (int64_t i = first; i <= last; ++i) {
-    const float* const src = part_of<BM, D>(p, i, i != first);
-    const float l = src[BM * D + jr], l_new = fmaxf(top, l);
-    float x[EL];
+  // `N` of them from i0 on, all on their way at once
+  auto add = [&](auto nn, int64_t i0) __attribute__((always_inline)) {
+    constexpr int N = decltype(nn)::value;
+    float l[N];
+    f32x4 x[N][EL / 4];
 #pragma unroll
-    for (int e = 0; e < EL; e += 4) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(src + jr * D + je + e);
+    for (int j = 0; j < N; ++j) {
+      const float* const src = part_of<BM, D>(p, i0 + j, i0 + j != first);
+      l[j] = src[BM * D + jr];
 #pragma unroll
-      for (int f = 0; f < 4; ++f) x[e + f] = y[f];
+      for (int e = 0; e < EL / 4; ++e) x[j][e] = *reinterpret_cast<const f32x4*>(src + jr * D + je + 4 * e);
     }
-    const float a = top == l_new ? 1.f : fast_exp2(top - l_new), w = l == l_new ? (l == -__builtin_inff() ? 0.f : 1.f) : fast_exp2(l - l_new);
-    total = total * a + w;
+    float l_new = top;
 #pragma unroll
-    for (int e = 0; e < EL; ++e) acc[e] = acc[e] * a + x[e] * w;
+    for (int j = 0; j < N; ++j) l_new = fmaxf(l_new, l[j]);
+    const float a = top == l_new ? 1.f : fast_exp2(top - l_new);
+    total *= a;
+#pragma unroll
+    for (int e = 0; e < EL; ++e) acc[e] *= a;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float w = l[j] == -__builtin_inff() ? 0.f : fast_exp2(l[j] - l_new);       // (parts without keys are zeros)
+      total += w;
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] += x[j][e / 4][e % 4] * w;
+    }
     top = l_new;
-  }
+  };
+  int64_t i = first;
+  for (; i + 7 <= last; i += 8) add(std::integral_constant<int, 8>{}, i);
+  if (i + 3 <= last) { add(std::integral_constant<int, 4>{}, i); i += 4; }
+  for (; i <= last; ++i) add(std::integral_constant<int, 1>{}, i);
   const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
   for (int e = 0; e < EL; ++e) acc[e] *= inv;

@@ -203,7 +203,7 @@ template <int BM, int BT>
 static void runs(const PagedAttn& p) {
   int64_t all = 0;
   for (int b = 0; b < p.c.n_seqs; ++b) { const PagedCost c = cost_of<BM, BT>(p, load_seq(p.c, b)); all += cost_upto(c, c.row_tiles) * p.c.Hkv; }
-  const int64_t share = larger<int64_t>((all + p.workers - 1) / p.workers, p.least_share);
+  const int64_t share = larger<int64_t>(static_cast<int64_t>(static_cast<double>(all) * p.by_workers) + 1, p.least_share);
   int64_t start = 0;
   for (int b = 0; b < p.c.n_seqs; ++b) {
     const PagedSeq s = load_seq(p.c, b);
@@ -211,7 +211,8 @@ static void runs(const PagedAttn& p) {
     for (int i = 0; i < c.row_tiles * p.c.Hkv; ++i) {
       const int64_t cost = c.first + i % c.row_tiles * c.step;
       const int tiles = rnd() % 50;
-      const int64_t first = (start + p.snap + share - 1) / share - 1, last = (start + cost - p.snap) / share;
+      const int64_t first = quotient(start + p.snap + share - 1, share) - 1, last = cost < p.snap ? -1 : quotient(start + cost - p.snap, share);
+      expect(first == (start + p.snap + share - 1) / share - 1, "quotient");
       const bool parts = cost >= 2 * p.snap && first < last;
       int upto = 0, takers = 0;
       for (int64_t w = larger<int64_t>(start / share - 1, 0); w <= (start + cost) / share; ++w) {
@@ -243,7 +244,7 @@ int main() {
     p.c.n_pages = 7; p.c.ps_log2 = ps_log2; p.c.Hkv = 2; p.c.n_seqs = n_seqs; p.c.max_pages = max_pages; p.c.n_rows = n_rows; p.c.cap = max_pages << ps_log2;
     p.G = 1 + rnd() % 9; p.tile_cost = 1; p.causal = rnd() % 4 != 0; p.window = p.causal && rnd() % 2 ? 1 + rnd() % 100 : 0; p.sinks = p.window ? rnd() % 70 : 0;
     if (p.window && rnd() % 5 == 0) { p.window = 1 << 30; p.sinks = 2147483647; }
-    p.workers = 1 + rnd() % 300; p.tile_cost = rnd() % 3000; p.snap = 1 + rnd() % 5000; p.least_share = 1 + rnd() % 9000;
+    p.workers = 1 + rnd() % 300; p.by_workers = 1.0 / p.workers; p.tile_cost = rnd() % 3000; p.snap = 1 + rnd() % 5000; p.least_share = 1 + rnd() % 9000;
     if (!wild) { runs<16, 128>(p); runs<128, 64>(p); runs<16, 64>(p); }
     tiles<16, 64>(p, table);
     tiles<16, 128>(p, table);
