@@ -27,7 +27,8 @@ struct RowsCfg {
   static constexpr int BM = 16, WK = 32;                 // rows of a tile; keys of a stage
   static constexpr int RB = D * (F8 ? 1 : 2);            // bytes of a row in the cache
   static constexpr int UNITS = RB / 16, RPL = 64 / UNITS, LOADS = WK / RPL;       // 16-byte units of it; rows to a wavefront's load; loads to a stage's K
-  static constexpr int NW = !F8 && D == 128 ? 2 : 4;     // wavefronts
+  static constexpr int NW = 2;                           // wavefronts
+  static constexpr int PER_CU = F8 ? (D == 128 ? 4 : 6) : (D == 128 ? 2 : 4);      // workgroups that a compute unit holds
   static constexpr int NS = 2;                           // stages in LDS
   static constexpr int BT = NW * WK;
   static constexpr int STAGE = 2 * WK * RB + (F8 ? 256 : 0), PER_STAGE = 2 * LOADS + (F8 ? 1 : 0);
@@ -59,7 +60,7 @@ typedef int i32x2v __attribute__((ext_vector_type(2)));
 typedef i32x2v __attribute__((address_space(3))) * lds_i32x2_ptr;
 
 template <int D, bool F8>
-__global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(const PagedAttn p) {
+__global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * RowsCfg<D, F8>::PER_CU / 4)) void paged_rows_kernel(const PagedAttn p) {
   using C = RowsCfg<D, F8>;
   constexpr int NW = C::NW, NS = C::NS, BT = C::BT, BM = C::BM, NDB = C::NDB, RB = C::RB;
   __shared__ __attribute__((aligned(256))) unsigned char smem[C::LDS];
@@ -71,13 +72,18 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
 
   PagedRun<BM, BT> run;
   const int worker = xcd_contiguous(blockIdx.x, p.workers);
-  if (!run.start(p, worker, lane)) return;
+  PagedSplit split{0, 0, 0, 0, worker, {0, 0, 0}};
+  if (!run.start(p, worker, lane)) {
+    leave_split<BM, BT>(p, worker, split);
+    return;
+  }
   const unsigned page_bytes = (static_cast<unsigned>(p.c.Hkv) << p.c.ps_log2) * RB;            // (below 2^31, the host sees to it)
   const int ps_mask = (1 << p.c.ps_log2) - 1;
   for (; run.next(p, lane); run.step()) {
     const PagedSeq& s = run.s;
     const int b = run.b, head = scalar(run.head), rt = scalar(run.rt);
     const bool whole = run.whole();
+    if (run.x0 == 0 && !whole) split = PagedSplit{run.s.r0, run.s.n * p.G, head, rt, run.last_worker(p, worker), {0, 0, 0}};
 
     // ---- the rows
     const int rows = s.n * p.G, m = rt * BM + lq, mc = min(m, rows - 1), tok = divide(mc, p.by_group);
@@ -368,24 +374,25 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64)) void paged_rows_kernel(c
     }
     __syncthreads();
   }
+  leave_split<BM, BT>(p, worker, split);
 }
+
+constexpr int kMostWorkers = 256 * 8;
 
 template <int D, bool F8>
-hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
+hipError_t launch_variant(PagedAttn p, hipStream_t stream) {
   using C = RowsCfg<D, F8>;
+  static_assert(256 * C::PER_CU <= kMostWorkers && C::PER_CU * (C::LDS + 4 * C::NW * C::LIST) <= 160 * 1024, "");
+  set_workers(p, 256 * C::PER_CU, C::BM, D);
   const hipError_t e = TASP_LAUNCH((paged_rows_kernel<D, F8>), dim3(static_cast<unsigned>(p.workers)), dim3(C::NW * 64), stream, p);
-  return e != hipSuccess ? e : launch_paged_combine<D, C::BM, C::BT>(p, stream);
+  return e != hipSuccess ? e : launch_paged_combine<D, C::BM>(p, stream);
 }
-
-constexpr int kWorkers = 512;
 
 }  // namespace
 
-int64_t paged_rows_workspace(int d) { return 2 * kWorkers * part_floats(16, d) * 4; }
+int64_t paged_rows_workspace(int d) { return workspace_of(kMostWorkers, 16, d); }
 
 hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
-  p.workers = kWorkers;
-  p.by_workers = 1.0 / p.workers;
   p.tile_cost = kParts / 4;
   p.snap = kParts / 4;
   p.least_share = kParts;

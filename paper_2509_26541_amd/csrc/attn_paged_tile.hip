@@ -60,7 +60,11 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
   const float c = p.scale_log2e;
   PagedRun<BM, BT> run;
   const int worker = xcd_contiguous(blockIdx.x, p.workers);
-  if (!run.start(p, worker, lane)) return;
+  PagedSplit split{0, 0, 0, 0, worker, {0, 0, 0}};
+  if (!run.start(p, worker, lane)) {
+    leave_split<BM, BT>(p, worker, split);
+    return;
+  }
 
   const unsigned page_bytes = (static_cast<unsigned>(p.c.Hkv) << p.c.ps_log2) * C::CB;          // (below 2^31, the host sees to it)
   const int ps_mask = (1 << p.c.ps_log2) - 1;
@@ -76,6 +80,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
   for (; run.next(p, lane); run.step()) {
     const int head = scalar(run.head), rt = scalar(run.rt), rows = run.s.n * p.G, left = rows - rt * BM;
     const bool whole = run.whole();
+    if (run.x0 == 0 && !whole) split = PagedSplit{run.s.r0, rows, head, rt, run.last_worker(p, worker), {0, 0, 0}};
     // The strip of 32 rows that a wavefront takes moves with the row tile: tiles with few rows leave strips without work.
     const int strip = (wave_u + rt) % NW;
     const int m = rt * BM + strip * 32 + lq, mc = min(m, rows - 1), tok = divide(mc, p.by_group);
@@ -517,6 +522,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
       }
     }
   }
+  leave_split<BM, BT>(p, worker, split);
 }
 
 constexpr int workers_of(int d) { return d == 64 ? 768 : 512; }       // three and two workgroups to a CU
@@ -525,16 +531,15 @@ template <int D, bool F8>
 hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
   using C = PTileCfg<D, F8>;
   const hipError_t e = TASP_LAUNCH((paged_tile_kernel<D, F8>), dim3(static_cast<unsigned>(p.workers)), dim3(C::NTHREADS), stream, p);
-  return e != hipSuccess ? e : launch_paged_combine<D, C::BM, C::BT>(p, stream);
+  return e != hipSuccess ? e : launch_paged_combine<D, C::BM>(p, stream);
 }
 
 }  // namespace
 
-int64_t paged_tile_workspace(int d) { return 2 * workers_of(d) * part_floats(128, d) * 4; }
+int64_t paged_tile_workspace(int d) { return workspace_of(workers_of(d), 128, d); }
 
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
-  p.workers = workers_of(d);
-  p.by_workers = 1.0 / p.workers;
+  set_workers(p, workers_of(d), 128, d);
   p.tile_cost = 2 * kParts;
   p.snap = 4 * kParts;
   p.least_share = 4 * kParts;

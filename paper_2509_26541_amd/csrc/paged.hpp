@@ -57,12 +57,17 @@ __host__ __device__ __forceinline__ PagedPlace place_of(const PagedView& p, int 
 __device__ __forceinline__ float scale_value(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // ---- attention: the rows (token, query head of the group) of a sequence and KV head in tiles of BM, their keys in tiles of BT
+// The row tile that a worker's run ends in, if others go on with it: its rows in the dense tensors, and the last of those workers (the
+// worker itself: there is none).
+struct PagedSplit { int32_t r0, rows, head, rt, last, unused[3]; };
+
 struct PagedAttn {
   PagedView c;
   const void* q;
   void* out;
   float* lse;
-  float* part;                   // workspace: partial results
+  float* part;                   // workspace: partial results, and
+  PagedSplit* split;             // of each worker, the row tile that it starts and others end
   int64_t q_stride;              // elements between the tokens of q
   int32_t Hq, G, causal, window, sinks, out_fp32;
   float scale_log2e;
@@ -282,6 +287,10 @@ struct PagedRun {
     ++rt;
   }
   __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == cost; }
+  // the last worker of a row tile that this one starts, for p.snap <= x1 < cost: runs end at `to` and every `share` behind it
+  __device__ __forceinline__ int last_worker(const PagedAttn& p, int worker) const {
+    return worker + 1 + static_cast<int>(quotient(at + cost - p.snap - to, share));
+  }
 };
 
 // A partial result: BM rows of d normalised sums, and their log-sum-exps to base 2.  A worker leaves at most two: of the row tile that its run

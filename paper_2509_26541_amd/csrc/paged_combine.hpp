@@ -2,8 +2,6 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <climits>
-
 #include "internal.hpp"
 #include "paged.hpp"
 #include "pipeline.hpp"
@@ -27,51 +25,36 @@ __device__ __forceinline__ void store_row(const PagedAttn& p, int64_t rh, int co
   if (col == 0) p.lse[rh] = lse2 * kLn2;
 }
 
-// A row tile whose keys several workgroups took: its partial results, in their order.  One workgroup to 16 rows of a row tile.
-template <int D, int BM, int BT>
+// What every worker leaves in p.split, once, at its end.
+template <int BM, int BT>
+__device__ __forceinline__ void leave_split(const PagedAttn& p, int worker, const PagedSplit& split) {
+  if (threadIdx.x == 0) p.split[worker] = split;
+}
+
+// A row tile whose keys several workgroups took: its partial results, in their order.  One workgroup to 16 rows of a row tile; where there are
+// fewer, the threads of the others take their turn of the parts.
+template <int D, int BM>
 __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
   constexpr int EL = D / 16, PER = BM / 16;
-  const int thread = threadIdx.x, lane = thread & 63;
-  PagedChunk<BM, BT> chunk;
-  const int64_t share = share_of<BM, BT>(p, chunk, lane);
-  int64_t unit = blockIdx.x / PER, start = 0;
-  int seq;
-  while (true) {
-    const int64_t upto = wave_prefix(static_cast<int64_t>(chunk.c.row_tiles) * p.c.Hkv);
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(upto > unit);
-    if (behind != 0) {
-      seq = __builtin_ctzll(behind);
-      if (seq > 0) unit -= of_lane(upto, seq - 1);
-      start += chunk.before(seq);
-      break;
-    }
-    unit -= of_lane(upto, 63);
-    start += chunk.before(64);
-    if (chunk.base + 64 >= p.c.n_seqs) return;
-    chunk.load(p, chunk.base + 64, lane);
-  }
-  const PagedCost c{static_cast<int>(__builtin_amdgcn_readlane(chunk.c.row_tiles, seq)), of_lane(chunk.c.first, seq), of_lane(chunk.c.step, seq)};
-  const int n = __builtin_amdgcn_readlane(chunk.s.n, seq), r0 = __builtin_amdgcn_readlane(chunk.s.r0, seq);
-  const int head = static_cast<int>(unit) / c.row_tiles, rt = static_cast<int>(unit) - head * c.row_tiles;
-  start += head * cost_upto(c, c.row_tiles) + cost_upto(c, rt);
-  const int64_t cost = c.first + rt * c.step;
-  // runs that end inside the row tile: those of workers first .. last - 1, ends snapped to neither side
-  if (cost < 2 * p.snap) return;
-  const int64_t first = quotient(start + p.snap + share - 1, share) - 1, last = quotient(start + cost - p.snap, share);
-  if (first >= last) return;
-  const int jr = blockIdx.x % PER * 16 + thread / 16, je = thread % 16 * EL, m = rt * BM + jr;
-  if (m >= n * p.G) return;
+  const int worker = blockIdx.x / PER, first_row = blockIdx.x % PER * 16;
+  const PagedSplit sp = p.split[worker];
+  const int m0 = sp.rt * BM + first_row;
+  if (sp.last == worker || m0 >= sp.rows) return;
+  const int here = min(sp.rows - m0, 16);                       // rows of this workgroup
+  const int turns = here > 8 ? 1 : here > 4 ? 2 : here > 2 ? 4 : here > 1 ? 8 : 16, per_turn = 16 / turns;
+  const int group = threadIdx.x / 16, je = threadIdx.x % 16 * EL, turn = group / per_turn, jr = first_row + min(group % per_turn, here - 1);
   float top = -__builtin_inff(), total = 0.f, acc[EL];
 #pragma unroll
   for (int e = 0; e < EL; ++e) acc[e] = 0.f;
-  // `N` of them from i0 on, all on their way at once
-  auto add = [&](auto nn, int64_t i0) __attribute__((always_inline)) {
+  // `N` parts from i0 on, every turns-th of them, all on their way at once
+  auto add = [&](auto nn, int i0) __attribute__((always_inline)) {
     constexpr int N = decltype(nn)::value;
     float l[N];
     f32x4 x[N][EL / 4];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float* const src = part_of<BM, D>(p, i0 + j, i0 + j != first);
+      const int i = i0 + j * turns;
+      const float* const src = part_of<BM, D>(p, i, i != worker);
       l[j] = src[BM * D + jr];
 #pragma unroll
       for (int e = 0; e < EL / 4; ++e) x[j][e] = *reinterpret_cast<const f32x4*>(src + jr * D + je + 4 * e);
@@ -92,22 +75,53 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
     }
     top = l_new;
   };
-  int64_t i = first;
-  for (; i + 7 <= last; i += 8) add(std::integral_constant<int, 8>{}, i);
-  if (i + 3 <= last) { add(std::integral_constant<int, 4>{}, i); i += 4; }
-  for (; i <= last; ++i) add(std::integral_constant<int, 1>{}, i);
+  int i = worker + turn;
+  for (; i + 7 * turns <= sp.last; i += 8 * turns) add(std::integral_constant<int, 8>{}, i);
+  if (i + 3 * turns <= sp.last) { add(std::integral_constant<int, 4>{}, i); i += 4 * turns; }
+  for (; i <= sp.last; i += turns) add(std::integral_constant<int, 1>{}, i);
+  if (turns > 1) {                                              // (the same for the whole workgroup)
+    __shared__ float sums[16][D + 4], tops[16], totals[16];
+#pragma unroll
+    for (int e = 0; e < EL; ++e) sums[group][je + e] = acc[e];
+    if (je == 0) { tops[group] = top; totals[group] = total; }
+    __syncthreads();
+    if (turn > 0) return;
+    float l_new = top;
+    for (int t = 1; t < turns; ++t) l_new = fmaxf(l_new, tops[t * per_turn + group]);
+    const float a = top == l_new ? 1.f : fast_exp2(top - l_new);
+    total *= a;
+#pragma unroll
+    for (int e = 0; e < EL; ++e) acc[e] *= a;
+    for (int t = 1; t < turns; ++t) {
+      const int other = t * per_turn + group;
+      const float w = tops[other] == -__builtin_inff() ? (totals[other] == 0.f ? 0.f : totals[other]) : fast_exp2(tops[other] - l_new);
+      total += w * totals[other];
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] += w * sums[other][je + e];
+    }
+    top = l_new;
+  }
+  const int m = m0 + group;
+  if (group >= here) return;
   const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
   for (int e = 0; e < EL; ++e) acc[e] *= inv;
   const int tok = divide(m, p.by_group);
-  store_row<D, EL>(p, static_cast<int64_t>(r0 + tok) * p.Hq + head * p.G + (m - tok * p.G), je, acc, top + __builtin_amdgcn_logf(total));
+  store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, top + __builtin_amdgcn_logf(total));
 }
 
-template <int D, int BM, int BT>
+template <int D, int BM>
 hipError_t launch_paged_combine(const PagedAttn& p, hipStream_t stream) {
-  const int64_t blocks = (static_cast<int64_t>(p.c.n_rows) * p.G / BM + p.c.n_seqs) * p.c.Hkv * (BM / 16);
-  if (blocks > INT_MAX) return hipErrorInvalidValue;
-  return TASP_LAUNCH((paged_combine_kernel<D, BM, BT>), dim3(static_cast<unsigned>(blocks)), dim3(256), stream, p);
+  return TASP_LAUNCH((paged_combine_kernel<D, BM>), dim3(static_cast<unsigned>(p.workers * (BM / 16))), dim3(256), stream, p);
+}
+
+// Bytes of the partial results of `workers` workgroups and of what they leave beside them, and where in a workspace these are.
+constexpr int64_t part_bytes(int workers, int bm, int d) { return (2 * workers * part_floats(bm, d) * 4 + 255) / 256 * 256; }
+constexpr int64_t workspace_of(int workers, int bm, int d) { return part_bytes(workers, bm, d) + workers * static_cast<int64_t>(sizeof(PagedSplit)); }
+inline void set_workers(PagedAttn& p, int workers, int bm, int d) {
+  p.workers = workers;
+  p.by_workers = 1.0 / workers;
+  p.split = reinterpret_cast<PagedSplit*>(reinterpret_cast<unsigned char*>(p.part) + part_bytes(workers, bm, d));
 }
 
 }  // namespace

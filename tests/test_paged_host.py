@@ -211,8 +211,7 @@ static void runs(const PagedAttn& p) {
     for (int i = 0; i < c.row_tiles * p.c.Hkv; ++i) {
       const int64_t cost = c.first + i % c.row_tiles * c.step;
       const int tiles = rnd() % 50;
-      const int64_t first = quotient(start + p.snap + share - 1, share) - 1, last = cost < p.snap ? -1 : quotient(start + cost - p.snap, share);
-      expect(first == (start + p.snap + share - 1) / share - 1, "quotient");
+      const int64_t first = (start + p.snap + share - 1) / share - 1, last = cost < p.snap ? -1 : (start + cost - p.snap) / share;
       const bool parts = cost >= 2 * p.snap && first < last;
       int upto = 0, takers = 0;
       for (int64_t w = larger<int64_t>(start / share - 1, 0); w <= (start + cost) / share; ++w) {
@@ -224,6 +223,8 @@ static void runs(const PagedAttn& p) {
         expect(parts ? w >= first && w <= last && (x0 == 0) == (w == first) : x0 == 0 && x1 == cost, "part");
         expect(key_tile_at(x0, cost, tiles) == upto, "gap");
         upto = key_tile_at(x1, cost, tiles);
+        // what the worker that starts a row tile says of the last one
+        if (parts && x0 == 0) expect(w + 1 + quotient(start + cost - p.snap - to, share) == last, "last worker");
         ++takers;
       }
       expect(upto == tiles && takers == (parts ? last - first + 1 : 1), "row tile not taken whole");
