@@ -28,7 +28,8 @@ int check_common(const tasp_paged_cache* c, const tasp_paged_batch* b, PagedView
   if (c->d != 64 && c->d != 128) return TASP_EUNSUPPORTED_SHAPE;
   if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0) return TASP_EUNSUPPORTED_SHAPE;
   if (c->n_pages > kMost || b->n_rows > kMost || static_cast<int64_t>(b->max_pages) * c->page_size > kMost) return TASP_EUNSUPPORTED_SHAPE;
-  if (static_cast<int64_t>(c->Hkv) * c->page_size * c->d * 2 >= (int64_t{1} << 31)) return TASP_EUNSUPPORTED_SHAPE;      // a page's bytes
+  if (static_cast<int64_t>(c->Hkv) * c->page_size * c->d * 2 >= (int64_t{1} << 31)) return TASP_EUNSUPPORTED_SHAPE;      // a page's bytes,
+  if (c->n_pages * c->Hkv * c->page_size >= (int64_t{1} << 32)) return TASP_EUNSUPPORTED_SHAPE;                                             // and all rows
   if (misaligned(c->k, 16) || misaligned(c->v, 16)) return TASP_EALIGN;
   if (e4m3 && (misaligned(c->k_scale, 16) || misaligned(c->v_scale, 16))) return TASP_EALIGN;
   if (misaligned(b->page_table, 4) || misaligned(b->kv_len, 4) || misaligned(b->row_start, 4)) return TASP_EALIGN;

@@ -70,7 +70,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
   const float c = p.scale_log2e;
   unsigned char* const ring = smem + w * NS * C::STAGE;
 
-  PagedRun<BM, BT> run;
+  PagedRun<BM, BT, true> run;
   const int worker = xcd_contiguous(blockIdx.x, p.workers);
   PagedSplit split{0, 0, 0, 0, worker, {0, 0, 0}};
   if (!run.start(p, worker, lane)) {

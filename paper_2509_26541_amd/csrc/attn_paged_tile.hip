@@ -45,10 +45,16 @@ __device__ __forceinline__ u32x4 widen8(unsigned a, unsigned b, float scale) {
   return r.v;
 }
 
+// One direct global->LDS load of 16 bytes per lane, as global_to_lds_16 with the fence, to `lds` + TO.
+template <int TO>
+__device__ __forceinline__ void lds_from(const unsigned char* base, unsigned off, unsigned lds) {
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base), "n"(TO) : "memory", "scc");
+}
+
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <int D, bool F8>
-__global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void paged_tile_kernel(const PagedAttn p) {
+__global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 2)) void paged_tile_kernel(const PagedAttn p) {
   using C = PTileCfg<D, F8>;
   constexpr int BM = C::BM, NW = C::NW, BT = C::BT, NDB = C::NDB, NJ = C::NJ, NL = C::PASSES;
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * C::TILE_BYTES];      // two K tiles, two V tiles
@@ -58,7 +64,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
   const int thread = threadIdx.x, wave_u = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int lane = thread & 63, h = lane >> 5, lq = lane & 31;
   const float c = p.scale_log2e;
-  PagedRun<BM, BT> run;
+  PagedRun<BM, BT, false> run;
   const int worker = xcd_contiguous(blockIdx.x, p.workers);
   PagedSplit split{0, 0, 0, 0, worker, {0, 0, 0}};
   if (!run.start(p, worker, lane)) {
@@ -66,7 +72,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
     return;
   }
 
-  const unsigned page_bytes = (static_cast<unsigned>(p.c.Hkv) << p.c.ps_log2) * C::CB;          // (below 2^31, the host sees to it)
+  const unsigned page_rows = static_cast<unsigned>(p.c.Hkv) << p.c.ps_log2;          // (all pages have fewer than 2^32, the host sees to it)
   const int ps_mask = (1 << p.c.ps_log2) - 1;
   const unsigned first_row = static_cast<unsigned>(C::row_of(wave_u) * C::CB);
   const unsigned lane_row = static_cast<unsigned>(lane / C::CUNITS);
@@ -77,7 +83,21 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
   const unsigned k_adr = lq * C::RB + C::swz_k(lq, h) * 16;          // unit 2 j + h sits at k_adr ^ 32 j
   const int vga = lane >> 4, vjj = lane & 15, vrow = 4 * (vga >> 1) + (vjj >> 2);
 
-  for (; run.next(p, lane); run.step()) {
+  // Workers of an XCD mostly have neighbouring row tiles of a KV head, whose keys they find in its L2 if they walk them together: a run starts
+  // with the row tiles that it has from their first key on, and a piece that starts inside one comes last.
+  bool piece = false, last_piece = false;
+  for (bool more = run.next(p, lane);;) {
+    if (!more) {
+      if (!piece || last_piece) break;
+      last_piece = true;
+      run.start(p, worker, lane);
+      run.next(p, lane);
+    } else if (run.x0 > 0 && !piece) {
+      piece = true;
+      run.step();
+      more = run.next(p, lane);
+      continue;
+    }
     const int head = scalar(run.head), rt = scalar(run.rt), rows = run.s.n * p.G, left = rows - rt * BM;
     const bool whole = run.whole();
     if (run.x0 == 0 && !whole) split = PagedSplit{run.s.r0, rows, head, rt, run.last_worker(p, worker), {0, 0, 0}};
@@ -88,66 +108,96 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
     PagedKeys keys = keys_of<BM, BT>(p, run.s, tok0, tok1);
     const int p0 = run.s.kv - run.s.n;
     const int see_to = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1), see_from = p.window > 0 ? p0 + tok - p.window + 1 : INT_MIN;
-    const int all_to = min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1), all_from = p.window > 0 ? p0 + tok1 - p.window + 1 : INT_MIN;
+    const int all_to = scalar(min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1)), all_from = scalar(p.window > 0 ? p0 + tok1 - p.window + 1 : INT_MIN);
     // (what the loader and the loop go by is the same in all lanes, and said to be)
     const int t0 = scalar(key_tile_at(run.x0, run.cost, keys.n_tiles)), n_tiles = scalar(key_tile_at(run.x1, run.cost, keys.n_tiles)) - t0;
     keys.n_first = scalar(keys.n_first);
     keys.from = scalar(keys.from);
     keys.end = scalar(keys.end);
 
-    // ---- loader.  Tiles are counted from t0.  list: pages of 16 tiles, from the last multiple of 8 on, one lane to 16 keys; -1 for none.
-    const int64_t head_bytes = (static_cast<int64_t>(head) << p.c.ps_log2) * C::CB;
-    const unsigned char* const k_head = p.c.k + head_bytes;
-    const unsigned char* const v_head = p.c.v + head_bytes;
+    // ---- loader.  Tiles are counted from t0.  For the 16 tiles from the last multiple of 8 on, one lane to 16 keys: list, the row of the
+    // pages where they start; paged, whether they have a page; easy, whether in addition every row sees all of them.
+    const uint64_t head_rows = static_cast<uint64_t>(head) << p.c.ps_log2;
+    const unsigned char* const k_base = p.c.k + head_rows * C::CB + first_row;
+    const unsigned char* const v_base = p.c.v + head_rows * C::CB + first_row;
     const int32_t* const table = p.c.table + static_cast<int64_t>(run.b) * p.c.max_pages;
     auto look_up = [&](int t) __attribute__((always_inline)) {
       const int u = t + lane / 4, pos = keys.tile(t0 + u) * BT + lane % 4 * 16;
       return u < n_tiles && pos < keys.end ? table[pos >> p.c.ps_log2] : -1;
     };
-    auto valid = [&](int page) __attribute__((always_inline)) { return page < p.c.n_pages ? page : -1; };      // (entries below 0 are left as they are)
-    int list = valid(look_up(0)), next = look_up(8);
-    uint64_t paged = __builtin_amdgcn_ballot_w64(list >= 0);
+    unsigned list;
+    uint64_t paged, easy;
+    auto take_list = [&](int t, int page) __attribute__((always_inline)) {
+      const int pos = keys.tile(t0 + t + lane / 4) * BT + lane % 4 * 16;
+      const bool has = page >= 0 && page < p.c.n_pages;
+      list = has ? static_cast<unsigned>(page) * page_rows + (pos & ps_mask) : 0u;
+      paged = __builtin_amdgcn_ballot_w64(has);
+      easy = __builtin_amdgcn_ballot_w64(has && pos + 15 <= all_to && (pos >= all_from || pos + 16 <= p.sinks));
+    };
+    take_list(0, look_up(0));
+    int next = look_up(8);
     auto turn_list = [&](int t) __attribute__((always_inline)) {
-      list = valid(next);
+      take_list(t, next);
       next = look_up(t + 8);
-      paged = __builtin_amdgcn_ballot_w64(list >= 0);
     };
-    // where the loads of a tile find their 16 keys: K's are made first, V's of the same tile a body later
-    int64_t at[NL];
-    unsigned records[NL];
+    auto is_easy = [&](int t, int listed) __attribute__((always_inline)) { return (static_cast<unsigned>(easy >> ((t - listed) * 4)) & 15) == 15; };
+    // Where the loads of a tile find their keys: K's are found first, V's of the same tile lie as far from v_base a body later.  An easy tile
+    // needs no more than that; otherwise each 16 keys have a descriptor, with as many records as count.
+    unsigned at[NL];
+    bool there = false;
     auto find = [&](int t, int listed) __attribute__((always_inline)) {
-      const int pos0 = keys.tile(t0 + t) * BT;
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int blk = C::block_of(wave_u, i), pos = pos0 + 16 * blk;
-        const int page = __builtin_amdgcn_readlane(list, (t - listed) * 4 + blk);
-        at[i] = static_cast<int64_t>(static_cast<uint64_t>(static_cast<unsigned>(max(page, 0))) * page_bytes) + static_cast<unsigned>((pos & ps_mask) * C::CB);
-        int n = min(16, keys.end - pos);
-        asm("" : "+s"(n));                       // (both bounds at once would be a vector instruction)
-        n = max(0, n);
-        records[i] = page < 0 ? 0u : static_cast<unsigned>(n) * C::CB;
-      }
+      for (int i = 0; i < NL; ++i) at[i] = __builtin_amdgcn_readlane(list, (t - listed) * 4 + C::block_of(wave_u, i));
+      there = is_easy(t, listed);
     };
-    // bf16: straight to LDS
-    auto fetch = [&](auto vv, int st) __attribute__((always_inline)) {
+    auto records_of = [&](int t, int listed, int i, uint64_t& row) __attribute__((always_inline)) {
+      const int place = (t - listed) * 4 + C::block_of(wave_u, i), pos = keys.tile(t0 + t) * BT + 16 * C::block_of(wave_u, i);
+      row = __builtin_amdgcn_readlane(list, place);
+      const int n = larger(0, scalar(lesser(16, keys.end - pos)));        // (both bounds at once would be a vector instruction)
+      return (paged >> place & 1) != 0 ? static_cast<unsigned>(n) : 0u;
+    };
+    // bf16: straight to LDS, of which the wavefront has the 1 KiB at `mine` of every pass.  (`t` and `listed` are looked at only for tiles that
+    // are not easy.)
+    const unsigned mine = smem_lds + wave_u * 1024;
+    auto fetch = [&](auto vv, auto ss, bool easy_tile, int t, int listed) __attribute__((always_inline)) {
       constexpr bool V = decltype(vv)::value;
-      unsigned char* const dst = smem + (V ? 2 * C::TILE_BYTES : 0) + st * C::TILE_BYTES + wave_u * 1024;
+      constexpr int TO = (V ? 2 * C::TILE_BYTES : 0) + decltype(ss)::value * C::TILE_BYTES;
+      if (__builtin_expect(easy_tile, 1)) {
+        static_for<NL>([&](auto i) __attribute__((always_inline)) {
+          lds_from<TO + decltype(i)::value * C::NTHREADS * 16>((V ? v_base : k_base) + static_cast<uint64_t>(at[decltype(i)::value]) * C::CB, V ? v_lane : k_lane, mine);
+        });
+      } else {
 #pragma unroll
-      for (int i = 0; i < NL; ++i)
-        buffer_to_lds_16<true>(raw_buffer((V ? v_head : k_head) + at[i], records[i]), min(first_row, records[i]), V ? v_lane : k_lane, dst + i * C::NTHREADS * 16);
+        for (int i = 0; i < NL; ++i) {
+          uint64_t row;
+          const unsigned records = records_of(t, listed, i, row) * C::CB;
+          buffer_to_lds_16<true>(raw_buffer((V ? v_base : k_base) - first_row + row * C::CB, records), lesser(first_row, records), V ? v_lane : k_lane,
+                                 smem + TO + wave_u * 1024 + i * C::NTHREADS * 16);
+        }
+      }
     };
     // e4m3: to registers, and from there, as bf16, to LDS
     u32x4 held[2][F8 ? NL : 1];
     unsigned held_scale[2][F8 ? NL : 1];
-    const int64_t head_rows = static_cast<int64_t>(head) << p.c.ps_log2;
-    auto load = [&](auto vv) __attribute__((always_inline)) {
+    auto load = [&](auto vv, bool easy_tile, int t, int listed) __attribute__((always_inline)) {
       constexpr bool V = decltype(vv)::value;
+      const unsigned char* const scales = (V ? p.c.v_scale : p.c.k_scale) + head_rows;
+      if (__builtin_expect(easy_tile, 1)) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>((V ? v_head : k_head) + at[i]), 0, static_cast<int>(records[i]), 0x00020000);
-        held[V][i] = __builtin_amdgcn_raw_buffer_load_b128(rs, static_cast<int>(first_row + (V ? v_lane : k_lane)), 0, 0);
-        const auto ss = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>((V ? p.c.v_scale : p.c.k_scale) + head_rows + at[i] / C::CB), 0, static_cast<int>(records[i] / C::CB), 0x00020000);
-        held_scale[V][i] = __builtin_amdgcn_raw_buffer_load_b8(ss, static_cast<int>(C::row_of(wave_u) + lane_row), 0, 0);
+        for (int i = 0; i < NL; ++i) {
+          held[V][i] = *reinterpret_cast<const u32x4*>((V ? v_base : k_base) + static_cast<uint64_t>(at[i]) * C::CB + k_lane);
+          held_scale[V][i] = (scales + at[i] + C::row_of(wave_u))[lane_row];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          uint64_t row;
+          const unsigned n = records_of(t, listed, i, row);
+          const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>((V ? v_base : k_base) - first_row + row * C::CB), 0, static_cast<int>(n * C::CB), 0x00020000);
+          held[V][i] = __builtin_amdgcn_raw_buffer_load_b128(rs, static_cast<int>(first_row + k_lane), 0, 0);
+          const auto ss = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(scales + row), 0, static_cast<int>(n), 0x00020000);
+          held_scale[V][i] = __builtin_amdgcn_raw_buffer_load_b8(ss, static_cast<int>(C::row_of(wave_u) + lane_row), 0, 0);
+        }
       }
     };
     auto put = [&](auto vv, int st) __attribute__((always_inline)) {
@@ -164,6 +214,8 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
     };
     constexpr std::false_type K{};
     constexpr std::true_type V{};
+    constexpr std::integral_constant<int, 0> stage0{};
+    constexpr std::integral_constant<int, 1> stage1{};
 
     u32x4 qf[NJ];
     {
@@ -173,13 +225,13 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
     }
     // K of tiles 0 and 1, V of tile 0
     if constexpr (F8) {
-      find(0, 0); load(K); load(V); put(K, 0); put(V, 0);
-      find(1, 0); load(K); put(K, 1);
-      load(V);                                     // V of tile 1, K of tile 2: written by body 0
-      find(2, 0); load(K);
+      find(0, 0); load(K, there, 0, 0); load(V, there, 0, 0); put(K, 0); put(V, 0);
+      find(1, 0); load(K, there, 1, 0); put(K, 1);
+      load(V, there, 1, 0);                        // V of tile 1, K of tile 2: written by body 0
+      find(2, 0); load(K, there, 2, 0);
     } else {
-      find(0, 0); fetch(K, 0); fetch(V, 0);
-      find(1, 0); fetch(K, 1);
+      find(0, 0); fetch(K, stage0, there, 0, 0); fetch(V, stage0, there, 0, 0);
+      find(1, 0); fetch(K, stage1, there, 1, 0);
     }
     unsigned ka[NJ], va[NDB];
 #pragma unroll
@@ -198,11 +250,12 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
     for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(qf[j]));
     __syncthreads();
     // What body t brings, V(t + 1) and K(t + 2): they go where body t - 1 has read last, and everybody has passed its barrier.
-    auto bring_v = [&](int st) __attribute__((always_inline)) {
-      if constexpr (F8) { put(V, st); load(V); } else fetch(V, st);
+    auto bring_v = [&](int t, auto ss) __attribute__((always_inline)) {
+      if constexpr (F8) { put(V, decltype(ss)::value); load(V, there, t + 2, t & ~7); } else fetch(V, ss, there, t + 1, t & ~7);
     };
-    auto bring_k = [&](int t, int st) __attribute__((always_inline)) {
-      if constexpr (F8) { put(K, st); find(t + 3, t & ~7); load(K); } else { find(t + 2, t & ~7); fetch(K, st); }
+    auto bring_k = [&](int t, auto ss) __attribute__((always_inline)) {
+      if constexpr (F8) { put(K, decltype(ss)::value); find(t + 3, t & ~7); load(K, there, t + 3, t & ~7); }
+      else { find(t + 2, t & ~7); fetch(K, ss, there, t + 2, t & ~7); }
     };
     auto brought = [&]() __attribute__((always_inline)) {
       if constexpr (!F8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -234,10 +287,9 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
     auto v_fragment = [&](auto ff) __attribute__((always_inline)) { constexpr int F = decltype(ff)::value % PD; return u32x4{fl[F][0], fl[F][1], fh[F][0], fh[F][1]}; };
     static_assert(NF % PD == 0 && NF % 2 == 0 && NV % 2 == 0 && PD % 2 == 0 && 4 * C::TILE_BYTES <= 65536, "");
     auto mask = [&](int t, int listed, f32x16 (&S)[2]) __attribute__((always_inline)) {
-      const int pos0 = keys.tile(t0 + t) * BT;
+      if (__builtin_expect(is_easy(t, listed), 1)) return;
       const unsigned has = static_cast<unsigned>(paged >> ((t - listed) * 4)) & 15;
-      if (__builtin_expect(has == 15 && pos0 + BT - 1 <= all_to && (pos0 >= all_from || pos0 + BT <= p.sinks), 1)) return;
-      const int at0 = pos0 + 4 * h;
+      const int at0 = keys.tile(t0 + t) * BT + 4 * h;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -317,8 +369,8 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
         read(std::integral_constant<int, F + PD>{}, sk, ss);
         exps(std::integral_constant<int, PRE + (EK - PRE) * F / NF>{}, std::integral_constant<int, PRE + (EK - PRE) * (F + 1) / NF>{}, S);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (F == 1) bring_v(ST ^ 1);
-        if constexpr (F == NF / 2 + 1) bring_k(t, ST);
+        if constexpr (F == 1) bring_v(t, sk);
+        if constexpr (F == NF / 2 + 1) bring_k(t, ss);
         __builtin_amdgcn_sched_barrier(0);
       });
       static_for<NV>([&](auto ff) __attribute__((always_inline)) {
@@ -355,15 +407,13 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
       add_up();
       fence_o();               // (here: the compiler may copy registers where the ways join)
     };
-    constexpr std::integral_constant<int, 0> stage0{};
-    constexpr std::integral_constant<int, 1> stage1{};
     const bool idle = strip * 32 >= left;
     if (idle) {                        // no rows: the loads only, with the barriers of the others
       if (n_tiles > 1) __syncthreads();
       for (int t = 0; t + 1 < n_tiles; ++t) {
         if ((t & 7) == 0 && t > 0) turn_list(t);
-        bring_v((t + 1) & 1);
-        bring_k(t, t & 1);
+        if (t % 2 == 0) { bring_v(t, stage1); bring_k(t, stage0); }
+        else { bring_v(t, stage0); bring_k(t, stage1); }
         brought();
       }
     } else if (n_tiles > 0) {
@@ -418,12 +468,11 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
       m_run = kNegBig; m_raise = kNegBig; l_run = 0.f; l_lo = 0.f; r_fix = 0.f;
       for (int t = 0; t < n_tiles; ++t) {
         if (t % 16 == 0) {
-          list = valid(look_up(t));
-          paged = __builtin_amdgcn_ballot_w64(list >= 0);
+          take_list(t, look_up(t));
         }
         find(t, t & ~15);
-        if constexpr (F8) { load(K); load(V); put(K, 0); put(V, 0); }
-        else { fetch(K, 0); fetch(V, 0); asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+        if constexpr (F8) { load(K, there, t, t & ~15); load(V, there, t, t & ~15); put(K, 0); put(V, 0); }
+        else { fetch(K, stage0, there, t, t & ~15); fetch(V, stage0, there, t, t & ~15); asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
         if (thread < BT) odd_rows[thread] = 0;
         __syncthreads();
         unsigned char* const mine = smem + 2 * C::TILE_BYTES + th * (C::TILE_BYTES / C::NTHREADS);      // a quarter of row thread / 4
@@ -521,11 +570,14 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), D == 64 ? 3 : 2) void 
         }
       }
     }
+    if (last_piece) break;
+    run.step();
+    more = run.next(p, lane);
   }
   leave_split<BM, BT>(p, worker, split);
 }
 
-constexpr int workers_of(int d) { return d == 64 ? 768 : 512; }       // three and two workgroups to a CU
+constexpr int workers_of(bool e4m3, int d) { return d == 64 && !e4m3 ? 768 : 512; }       // three and two workgroups to a CU
 
 template <int D, bool F8>
 hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
@@ -536,10 +588,10 @@ hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
 
 }  // namespace
 
-int64_t paged_tile_workspace(int d) { return workspace_of(workers_of(d), 128, d); }
+int64_t paged_tile_workspace(int d) { return workspace_of(workers_of(false, d), 128, d); }
 
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
-  set_workers(p, workers_of(d), 128, d);
+  set_workers(p, workers_of(e4m3, d), 128, d);
   p.tile_cost = 2 * kParts;
   p.snap = 4 * kParts;
   p.least_share = 4 * kParts;

@@ -114,6 +114,11 @@ __host__ __device__ __forceinline__ PagedCost cost_of(const PagedAttn& p, const 
     }
   }
   c.first = keys * (kParts / BT) + p.tile_cost;
+  // Row tiles that differ little count as equal: where there is one to a worker, no run ends inside.
+  if (c.step * c.row_tiles <= c.first / 8) {
+    c.first += c.step * c.row_tiles / 2;
+    c.step = 0;
+  }
   return c;
 }
 // About 1 / x, and a / b rounded down (0 <= a < 2^52, b > 0): the compiler's 64-bit division is some 150 dependent instructions.
@@ -205,8 +210,9 @@ __device__ __forceinline__ int64_t share_of(const PagedAttn& p, PagedChunk<BM, B
   return uniform(larger<int64_t>(static_cast<int64_t>(static_cast<double>(all) * p.by_workers) + 1, p.least_share));
 }
 
-// A worker's run of the call's work, one row tile (or piece of one) after the other.
-template <int BM, int BT>
+// A worker's run of the call's work, one row tile (or piece of one) after the other.  KEEP: the lists of the chunk stay in registers
+// (a dozen of them); otherwise those of a sequence are read again when its turn comes.
+template <int BM, int BT, bool KEEP>
 struct PagedRun {
   PagedChunk<BM, BT> chunk;
   int64_t share, from, to;       // the run, in parts from the start of sequence `seq` of the chunk
@@ -217,14 +223,22 @@ struct PagedRun {
   int64_t x0, x1;                // what the run has of it
   int b;
 
-  __device__ __forceinline__ void take() {
-    s.n = __builtin_amdgcn_readlane(chunk.s.n, seq);
-    s.kv = __builtin_amdgcn_readlane(chunk.s.kv, seq);
-    s.r0 = __builtin_amdgcn_readlane(chunk.s.r0, seq);
-    c.row_tiles = __builtin_amdgcn_readlane(chunk.c.row_tiles, seq);
-    c.first = of_lane(chunk.c.first, seq);
-    c.step = of_lane(chunk.c.step, seq);
-    b = chunk.base + seq;
+  __device__ __forceinline__ void take(const PagedAttn& p) {
+    if constexpr (KEEP) {
+      s.n = __builtin_amdgcn_readlane(chunk.s.n, seq);
+      s.kv = __builtin_amdgcn_readlane(chunk.s.kv, seq);
+      s.r0 = __builtin_amdgcn_readlane(chunk.s.r0, seq);
+      c.row_tiles = __builtin_amdgcn_readlane(chunk.c.row_tiles, seq);
+      c.first = of_lane(chunk.c.first, seq);
+      c.step = of_lane(chunk.c.step, seq);
+      b = chunk.base + seq;
+    } else {
+      const PagedSeq one = load_seq(p.c, b);
+      s.n = __builtin_amdgcn_readfirstlane(one.n);
+      s.kv = __builtin_amdgcn_readfirstlane(one.kv);
+      s.r0 = __builtin_amdgcn_readfirstlane(one.r0);
+      c = cost_of<BM, BT>(p, s);
+    }
   }
   // false: no work for this worker
   __device__ __forceinline__ bool start(const PagedAttn& p, int worker, int lane) {
@@ -246,7 +260,8 @@ struct PagedRun {
       if (chunk.base + 64 >= p.c.n_seqs) return false;
       chunk.load(p, chunk.base + 64, lane);
     }
-    take();
+    b = chunk.base + seq;
+    take(p);
     const int64_t one = cost_upto(c, c.row_tiles);
     head = static_cast<int>(quotient(from, one));
     rt = row_tile_at(c, from - head * one);
@@ -265,13 +280,13 @@ struct PagedRun {
         from -= at;
         to -= at;
         at = 0;
-        if (++seq == 64) {
-          if (chunk.base + 64 >= p.c.n_seqs) return false;
-          chunk.load(p, chunk.base + 64, lane);
-          seq = 0;
-        }
-        if (chunk.base + seq >= p.c.n_seqs) return false;
-        take();
+        if (++b >= p.c.n_seqs) return false;
+        if constexpr (KEEP)
+          if (++seq == 64) {
+            chunk.load(p, chunk.base + 64, lane);
+            seq = 0;
+          }
+        take(p);
         continue;
       }
       cost = c.first + rt * c.step;

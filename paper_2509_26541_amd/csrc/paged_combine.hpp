@@ -31,15 +31,17 @@ __device__ __forceinline__ void leave_split(const PagedAttn& p, int worker, cons
   if (threadIdx.x == 0) p.split[worker] = split;
 }
 
-// A row tile whose keys several workgroups took: its partial results, in their order.  One workgroup to 16 rows of a row tile; where there are
-// fewer, the threads of the others take their turn of the parts.
+// A row tile whose keys several workgroups took: its partial results, in their order, 16 rows at a time (and up to 64 to a workgroup).  Where
+// there are fewer, the threads of the others take their turn of the parts.
 template <int D, int BM>
 __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
-  constexpr int EL = D / 16, PER = BM / 16;
-  const int worker = blockIdx.x / PER, first_row = blockIdx.x % PER * 16;
+  constexpr int EL = D / 16, ROWS = BM < 64 ? BM : 64, PER = BM / ROWS;
+  const int worker = blockIdx.x / PER;
   const PagedSplit sp = p.split[worker];
+  if (sp.last == worker) return;
+  for (int first_row = blockIdx.x % PER * ROWS, end_row = first_row + ROWS; first_row < end_row; first_row += 16) {
   const int m0 = sp.rt * BM + first_row;
-  if (sp.last == worker || m0 >= sp.rows) return;
+  if (m0 >= sp.rows) return;
   const int here = min(sp.rows - m0, 16);                       // rows of this workgroup
   const int turns = here > 8 ? 1 : here > 4 ? 2 : here > 2 ? 4 : here > 1 ? 8 : 16, per_turn = 16 / turns;
   const int group = threadIdx.x / 16, je = threadIdx.x % 16 * EL, turn = group / per_turn, jr = first_row + min(group % per_turn, here - 1);
@@ -85,7 +87,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
     for (int e = 0; e < EL; ++e) sums[group][je + e] = acc[e];
     if (je == 0) { tops[group] = top; totals[group] = total; }
     __syncthreads();
-    if (turn > 0) return;
+    if (turn > 0) return;                                       // (a row tile's last rows)
     float l_new = top;
     for (int t = 1; t < turns; ++t) l_new = fmaxf(l_new, tops[t * per_turn + group]);
     const float a = top == l_new ? 1.f : fast_exp2(top - l_new);
@@ -102,17 +104,18 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
     top = l_new;
   }
   const int m = m0 + group;
-  if (group >= here) return;
+  if (group >= here) return;                                    // (so are these)
   const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
   for (int e = 0; e < EL; ++e) acc[e] *= inv;
   const int tok = divide(m, p.by_group);
   store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, top + __builtin_amdgcn_logf(total));
+  }
 }
 
 template <int D, int BM>
 hipError_t launch_paged_combine(const PagedAttn& p, hipStream_t stream) {
-  return TASP_LAUNCH((paged_combine_kernel<D, BM>), dim3(static_cast<unsigned>(p.workers * (BM / 16))), dim3(256), stream, p);
+  return TASP_LAUNCH((paged_combine_kernel<D, BM>), dim3(static_cast<unsigned>(p.workers * (BM < 64 ? 1 : BM / 64))), dim3(256), stream, p);
 }
 
 // Bytes of the partial results of `workers` workgroups and of what they leave beside them, and where in a workspace these are.
