@@ -374,8 +374,8 @@ double tasp_chunk_attn_bwd_flops(const tasp_schedule_t* s, const tasp_attn_bwd_a
  *   k, v      [n_pages, Hkv, page_size, d]: a head's rows of a page lie together.  page_size a power of
  *             two from 16 to 1024, d 64 or 128.
  *   dtype     TASP_DTYPE_BF16, or TASP_DTYPE_E4M3 (8-bit floats without infinities, largest value 448).
- *   k_scale,  [n_pages, Hkv, page_size] bytes, TASP_DTYPE_E4M3 only: byte b of a row stands for the factor
- *   v_scale   2^(b - 127) of its d values (b = 0: 0).
+ *   k_scale,  [n_pages, Hkv, page_size] bytes, TASP_DTYPE_E4M3 only: byte b <= 254 of a row stands for the factor
+ *   v_scale   2^(b - 127) of its d values (b = 0: 0).  255 is no factor: it may make any row of its sequence NaN.
  *
  * The batch (tasp_paged_batch; the three lists are device memory, 4-byte aligned, read when the kernels run):
  *   row_start [n_seqs + 1]  not falling; rows row_start[b] .. row_start[b+1] - 1 of the dense tensors are

@@ -1,4 +1,4 @@
-// Attention of a few new tokens over a paged cache: 16 (token, query head of the group) rows to a tile.
+// Attention of a few new tokens over a paged cache: 16 or 32 (token, query head of the group) rows to a tile.
 //
 // S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, softmax in one pass (running maximum and sum).  A grouped head's K and V
 // are read once for all 16 rows.  Every wavefront takes keys of its own, in stages of 32, through a part of LDS of its own that loads
@@ -22,19 +22,20 @@
 namespace tasp {
 namespace {
 
-template <int D, bool F8>
+// NR times 16 rows to a tile.
+template <int D, bool F8, int NR>
 struct RowsCfg {
-  static constexpr int BM = 16, WK = 32;                 // rows of a tile; keys of a stage
+  static constexpr int BM = 16 * NR, WK = 32;            // rows of a tile; keys of a stage
   static constexpr int RB = D * (F8 ? 1 : 2);            // bytes of a row in the cache
   static constexpr int UNITS = RB / 16, RPL = 64 / UNITS, LOADS = WK / RPL;       // 16-byte units of it; rows to a wavefront's load; loads to a stage's K
   static constexpr int NW = 2;                           // wavefronts
-  static constexpr int PER_CU = F8 ? (D == 128 ? 4 : 6) : (D == 128 ? 2 : 4);      // workgroups that a compute unit holds
+  static constexpr int PER_CU = F8 ? (D == 128 || NR == 2 ? 4 : 6) : (D == 128 ? 2 : 4);      // workgroups that a compute unit holds
   static constexpr int NS = 2;                           // stages in LDS
   static constexpr int BT = NW * WK;
   static constexpr int STAGE = 2 * WK * RB + (F8 ? 256 : 0), PER_STAGE = 2 * LOADS + (F8 ? 1 : 0);
   static constexpr int LIST = 256;                       // pages a wavefront looks up at once, one for every 16 keys
   static constexpr int ROW = D + 4;                      // floats of a row of sums while they are joined
-  static constexpr int RING = NW * NS * STAGE, JOIN = NW * BM * ROW * 4 + NW * BM * 8, LDS = RING > JOIN ? RING : JOIN;
+  static constexpr int RING = NW * NS * STAGE, JOIN = NW * 16 * ROW * 4 + NW * 16 * 8, LDS = RING > JOIN ? RING : JOIN;
   static constexpr int NDB = D / 16;
   // 16-byte units of a stage's row are kept at unit ^ swz: the 16 rows that one read takes a unit (K) or two (V) of then lie in different banks
   __device__ static int swz_k(int r) { return (r / (16 / UNITS)) % UNITS; }
@@ -59,9 +60,9 @@ __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirst
 typedef int i32x2v __attribute__((ext_vector_type(2)));
 typedef i32x2v __attribute__((address_space(3))) * lds_i32x2_ptr;
 
-template <int D, bool F8>
-__global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * RowsCfg<D, F8>::PER_CU / 4)) void paged_rows_kernel(const PagedAttn p) {
-  using C = RowsCfg<D, F8>;
+template <int D, bool F8, int NR>
+__global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>::NW * RowsCfg<D, F8, NR>::PER_CU / 4)) void paged_rows_kernel(const PagedAttn p) {
+  using C = RowsCfg<D, F8, NR>;
   constexpr int NW = C::NW, NS = C::NS, BT = C::BT, BM = C::BM, NDB = C::NDB, RB = C::RB;
   __shared__ __attribute__((aligned(256))) unsigned char smem[C::LDS];
   __shared__ int pages[NW][C::LIST];
@@ -86,21 +87,24 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
     if (run.x0 == 0 && !whole) split = PagedSplit{run.s.r0, run.s.n * p.G, head, rt, run.last_worker(p, worker), {0, 0, 0}};
 
     // ---- the rows
-    const int rows = s.n * p.G, m = rt * BM + lq, mc = min(m, rows - 1), tok = divide(mc, p.by_group);
+    const int rows = s.n * p.G;
     const int tok0 = divide(rt * BM, p.by_group), tok1 = divide(min(rt * BM + BM, rows) - 1, p.by_group);
     PagedKeys keys = keys_of<BM, BT>(p, s, tok0, tok1);
     const int p0 = s.kv - s.n;
-    const int see_to = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1);         // the lane's row sees keys up to it,
-    const int see_from = p.window > 0 ? p0 + tok - p.window + 1 : INT_MIN;       // from this one on or among the first
     const int all_to = min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1), all_from = p.window > 0 ? p0 + tok1 - p.window + 1 : INT_MIN;
-    bf16x8 qf[D / 32];
-    {
-      const __bf16* const src = static_cast<const __bf16*>(p.q) + static_cast<int64_t>(s.r0 + tok) * p.q_stride + static_cast<int64_t>(head * p.G + mc - tok * p.G) * D;
+    int see_to[NR], see_from[NR];                  // the lane's rows see keys up to the one, from the other on or among the first
+    bf16x8 qf[NR][D / 32];
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) qf[j] = *reinterpret_cast<const bf16x8*>(src + (F8 ? 64 * (j / 2) + 16 * g + 8 * (j % 2) : 32 * j + 8 * g));
+    for (int n = 0; n < NR; ++n) {
+      const int m = min(rt * BM + 16 * n + lq, rows - 1), tok = divide(m, p.by_group);
+      see_to[n] = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1);
+      see_from[n] = p.window > 0 ? p0 + tok - p.window + 1 : INT_MIN;
+      const __bf16* const src = static_cast<const __bf16*>(p.q) + static_cast<int64_t>(s.r0 + tok) * p.q_stride + static_cast<int64_t>(head * p.G + m - tok * p.G) * D;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) qf[n][j] = *reinterpret_cast<const bf16x8*>(src + (F8 ? 64 * (j / 2) + 16 * g + 8 * (j % 2) : 32 * j + 8 * g));
     }
-    f32x4 o[NDB];
-    float m_run, l_run, l_lo;
+    f32x4 o[NR][NDB];
+    float m_run[NR], l_run[NR], l_lo[NR];
 
     // (what the loads and the loop go by is the same in all lanes, and said to be)
     const int t0 = scalar(key_tile_at(run.x0, run.cost, keys.n_tiles)), t1 = scalar(key_tile_at(run.x1, run.cost, keys.n_tiles));
@@ -167,14 +171,20 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
     // times an infinity, is NaN for those that do.  Sums that are not finite are formed again, with the rows of V that hold
     // such values taken out of the product and added one by one.
     auto pass = [&](auto careful) {
+      float m_raise[NR];
 #pragma unroll
-      for (int i = 0; i < NDB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m_run = kNegBig; l_run = 0.f; l_lo = 0.f;
-      float m_raise = kNegBig;
+      for (int n = 0; n < NR; ++n) {
+#pragma unroll
+        for (int i = 0; i < NDB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m_run[n] = m_raise[n] = kNegBig;
+        l_run[n] = l_lo[n] = 0.f;
+      }
       if (t0 < t1) {
         look_up(t0);
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) asm volatile("" : "+v"(qf[j]));          // (the compiler waits for them here, not in the loop)
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) asm volatile("" : "+v"(qf[n][j]));     // (the compiler waits for them here, not in the loop)
         for (int i = 0; i < NS; ++i) fetch(t0 + i, i, listed_pages(t0 + i));
       }
       for (int t = t0, st = 0; t < t1; ++t, st = st + 1 == NS ? 0 : st + 1) {
@@ -184,22 +194,27 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
         unsigned char* const vl = ring + st * C::STAGE + C::WK * RB;
         const int pos0 = keys.tile(t) * BT + w * C::WK;
         const unsigned has = paged >> (2 * (NS - 1)) & 3;
-        // ---- scores: those of keys 4 g .. 4 g + 3 and 16 + 4 g .. of the lane's row
-        float x[8], vs[8];
+        // ---- scores: those of keys 4 g .. 4 g + 3 and 16 + 4 g .. of the lane's rows
+        float x[NR][8], vs[8];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          f32x4 sc = f32x4{0.f, 0.f, 0.f, 0.f};
+          f32x4 sc[NR];
+#pragma unroll
+          for (int n = 0; n < NR; ++n) sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
           const int r = 16 * i + lq;
+          auto product = [&](bf16x8 kf, int j) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][j], sc[n], 0, 0, 0);
+          };
           if constexpr (!F8) {
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-              sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(kl + r * RB + ((4 * j + g) ^ C::swz_k(r)) * 16), qf[j], sc, 0, 0, 0);
+            for (int j = 0; j < D / 32; ++j) product(*reinterpret_cast<const bf16x8*>(kl + r * RB + ((4 * j + g) ^ C::swz_k(r)) * 16), j);
           } else {
 #pragma unroll
             for (int j = 0; j < D / 64; ++j) {
               const u32x4 k16 = *reinterpret_cast<const u32x4*>(kl + r * RB + ((4 * j + g) ^ C::swz_k(r)) * 16);
-              sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2{k16[0], k16[1]}), qf[2 * j], sc, 0, 0, 0);
-              sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2{k16[2], k16[3]}), qf[2 * j + 1], sc, 0, 0, 0);
+              product(widen(u32x2{k16[0], k16[1]}), 2 * j);
+              product(widen(u32x2{k16[2], k16[3]}), 2 * j + 1);
             }
           }
           if constexpr (F8) {
@@ -207,51 +222,63 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
             const unsigned vw = *reinterpret_cast<const unsigned*>(kl + 2 * C::WK * RB + 32 + 16 * i + 4 * g);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              x[4 * i + e] = sc[e] * scale_value(kw >> 8 * e & 255);
+              const float ks = scale_value(kw >> 8 * e & 255);
+#pragma unroll
+              for (int n = 0; n < NR; ++n) x[n][4 * i + e] = sc[n][e] * ks;
               vs[4 * i + e] = scale_value(vw >> 8 * e & 255);
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * i + e] = sc[e];
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[n][4 * i + e] = sc[n][e];
           }
         }
-        unsigned seen = 0xff;
+        unsigned seen[NR];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) seen[n] = 0xff;
         if (!(has == 3 && pos0 + C::WK - 1 <= all_to && (pos0 >= all_from || pos0 + C::WK <= p.sinks))) {
-          seen = 0;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const int pos = pos0 + 16 * (e / 4) + 4 * g + e % 4;
-            const bool ok = (has >> (e / 4) & 1) != 0 && pos <= see_to && (pos >= see_from || pos < p.sinks);
-            seen |= ok ? 1u << e : 0u;
-            x[e] = ok ? x[e] : -__builtin_inff();
-            if constexpr (F8) vs[e] = ok ? vs[e] : 0.f;          // (a scale behind the end may be anything)
+            const bool there = (has >> (e / 4) & 1) != 0 && pos < keys.end;
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              const bool ok = there && pos <= see_to[n] && (pos >= see_from[n] || pos < p.sinks);
+              seen[n] &= ok ? 0xffu : ~(1u << e);
+              x[n][e] = ok ? x[n][e] : -__builtin_inff();
+            }
+            if constexpr (F8) vs[e] = there ? vs[e] : 0.f;       // (a scale behind the end may be anything)
           }
         }
-        // ---- softmax: the running maximum is only raised when it grew by more than 2^8
-        const float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        if (__builtin_amdgcn_ballot_w64(mx * c > m_raise) != 0) {
-          float m_new = fmaxf(mx, __shfl_xor(mx, 16));
-          m_new = fmaxf(m_run, fmaxf(m_new, __shfl_xor(m_new, 32)) * c);
-          const float alpha = fast_exp2(m_run - m_new);
-          m_run = m_new;
-          m_raise = m_new + kRescaleGap;
-          l_run *= alpha; l_lo *= alpha;
+        bf16x8 hi[NR], lo[NR];
 #pragma unroll
-          for (int i = 0; i < NDB; ++i) o[i] *= alpha;
-        }
-        bf16x8 hi, lo;
-        float sum = 0.f;
+        for (int n = 0; n < NR; ++n) {
+          // ---- softmax: the running maximum is only raised when it grew by more than 2^8
+          const float mx = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])), fmaxf(fmaxf(x[n][4], x[n][5]), fmaxf(x[n][6], x[n][7])));
+          if (__builtin_amdgcn_ballot_w64(mx * c > m_raise[n]) != 0) {
+            float m_new = fmaxf(mx, __shfl_xor(mx, 16));
+            m_new = fmaxf(m_run[n], fmaxf(m_new, __shfl_xor(m_new, 32)) * c);
+            const float alpha = fast_exp2(m_run[n] - m_new);
+            m_run[n] = m_new;
+            m_raise[n] = m_new + kRescaleGap;
+            l_run[n] *= alpha; l_lo[n] *= alpha;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = fast_exp2(__builtin_fmaf(x[e], c, -m_run));
-          sum += x[e];
-          if constexpr (F8) x[e] *= vs[e];
-          hi[e] = static_cast<__bf16>(x[e]);
-          lo[e] = static_cast<__bf16>(x[e] - static_cast<float>(hi[e]));
+            for (int i = 0; i < NDB; ++i) o[n][i] *= alpha;
+          }
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[n][e] = fast_exp2(__builtin_fmaf(x[n][e], c, -m_run[n]));
+            sum += x[n][e];
+            if constexpr (F8) x[n][e] *= vs[e];
+            hi[n][e] = static_cast<__bf16>(x[n][e]);
+            lo[n][e] = static_cast<__bf16>(x[n][e] - static_cast<float>(hi[n][e]));
+          }
+          // in two levels, so that a few large terms do not swallow many small ones
+          l_lo[n] += sum;
+          if ((t & 63) == 63) { l_run[n] += l_lo[n]; l_lo[n] = 0.f; }
         }
-        // in two levels, so that a few large terms do not swallow many small ones
-        l_lo += sum;
-        if ((t & 63) == 63) { l_run += l_lo; l_lo = 0.f; }
 
         if constexpr (decltype(careful)::value) {
           // (places formed here: outside the loop they would take registers from it)
@@ -278,11 +305,16 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
           while (rows_odd != 0) {
             const int r = __builtin_ctzll(rows_odd) / 2, at_e = r / 16 * 4 + r % 4, from_lane = r % 16 / 4 * 16 + cq;
             rows_odd &= rows_odd - 1;
-            float pr = 0.f;
+            float pr[NR];
+            bool sees[NR];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pr = e == at_e ? x[e] : pr;
-            pr = __shfl(pr, from_lane);
-            const bool sees = (__shfl(static_cast<int>(seen), from_lane) >> at_e & 1) != 0;
+            for (int n = 0; n < NR; ++n) {
+              float mine = 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) mine = e == at_e ? x[n][e] : mine;
+              pr[n] = __shfl(mine, from_lane);
+              sees[n] = (__shfl(static_cast<int>(seen[n]), from_lane) >> at_e & 1) != 0;
+            }
 #pragma unroll
             for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -295,7 +327,8 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
                 } else {
                   y = static_cast<float>(*reinterpret_cast<const __bf16*>(vl + r * RB + ((col / 8) ^ C::swz_v(r)) * 16 + col % 8 * 2));
                 }
-                o[db][e] += sees ? pr * y : 0.f;
+#pragma unroll
+                for (int n = 0; n < NR; ++n) o[n][db][e] += sees[n] ? pr[n] * y : 0.f;
               }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (ln < C::UNITS) *reinterpret_cast<u32x4*>(vl + r * RB + ln * 16) = u32x4{0u, 0u, 0u, 0u};
@@ -313,8 +346,10 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
             const int r8 = lq >> 1, r = 4 * g + (r8 & 3) + (r8 >> 2) * 16;
             vf = widen(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_ptr)(lds_void_ptr)(vl + r * RB + (db ^ C::swz_v(r)) * 16 + 8 * (lq & 1)))));
           }
-          o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi, o[db], 0, 0, 0);
-          o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo, o[db], 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) o[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[n], o[n][db], 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) o[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[n], o[n][db], 0, 0, 0);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the stage has been read
         fetch(t + NS, st, soon);
@@ -325,51 +360,57 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
     {
       float z = 0.f;
 #pragma unroll
-      for (int i = 0; i < NDB; ++i)
+      for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[i][e], 0.f, z);
+        for (int i = 0; i < NDB; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[n][i][e], 0.f, z);
       if (__builtin_expect(__builtin_amdgcn_ballot_w64(z != 0.f) != 0, 0)) pass(std::true_type{});       // (0 times a number is 0)
     }
 
-    // ---- the wavefronts' sums are joined
-    float l = l_run + l_lo;
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    // ---- the wavefronts' sums are joined, 16 rows at a time
     float* const sums = reinterpret_cast<float*>(smem);
-    float* const tops = sums + NW * BM * C::ROW;
-    __syncthreads();
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(sums + (w * BM + lq) * C::ROW + 16 * db + 4 * g) = o[db];
-    if (g == 0) { tops[w * BM + lq] = m_run; tops[(NW + w) * BM + lq] = l; }
-    __syncthreads();
-    constexpr int TPR = NW * 64 / BM, EL = D / TPR;              // threads to a row, and its values to each
+    float* const tops = sums + NW * 16 * C::ROW;
+    constexpr int TPR = NW * 64 / 16, EL = D / TPR;              // threads to a row, and its values to each
     const int jr = thread / TPR, je = thread % TPR * EL;
-    float top = kNegBig, weight[NW], total = 0.f, acc[EL];
 #pragma unroll
-    for (int i = 0; i < NW; ++i) top = fmaxf(top, tops[i * BM + jr]);
+    for (int n = 0; n < NR; ++n) {
+      float l = l_run[n] + l_lo[n];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      weight[i] = fast_exp2(tops[i * BM + jr] - top);
-      total += weight[i] * tops[(NW + i) * BM + jr];
-    }
+      for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(sums + (w * 16 + lq) * C::ROW + 16 * db + 4 * g) = o[n][db];
+      if (g == 0) { tops[w * 16 + lq] = m_run[n]; tops[(NW + w) * 16 + lq] = l; }
+      __syncthreads();
+      float top = kNegBig, weight[NW], total = 0.f, acc[EL];
 #pragma unroll
-    for (int e = 0; e < EL; ++e) acc[e] = 0.f;
+      for (int i = 0; i < NW; ++i) top = fmaxf(top, tops[i * 16 + jr]);
 #pragma unroll
-    for (int i = 0; i < NW; ++i)
+      for (int i = 0; i < NW; ++i) {
+        weight[i] = fast_exp2(tops[i * 16 + jr] - top);
+        total += weight[i] * tops[(NW + i) * 16 + jr];
+      }
 #pragma unroll
-      for (int e = 0; e < EL; ++e) acc[e] += weight[i] * sums[(i * BM + jr) * C::ROW + je + e];
-    const float inv = total == 0.f ? 0.f : 1.f / total, lse2 = total == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(total);
+      for (int e = 0; e < EL; ++e) acc[e] = 0.f;
 #pragma unroll
-    for (int e = 0; e < EL; ++e) acc[e] *= inv;
-    if (rt * BM + jr < rows) {
-      if (whole) {
-        const int jt = divide(rt * BM + jr, p.by_group);
-        store_row<D, EL>(p, static_cast<int64_t>(s.r0 + jt) * p.Hq + head * p.G + (rt * BM + jr - jt * p.G), je, acc, lse2);
-      } else {
-        float* const dst = part_of<BM, D>(p, worker, run.x0 > 0);
+      for (int i = 0; i < NW; ++i)
 #pragma unroll
-        for (int e = 0; e < EL; e += 4) *reinterpret_cast<f32x4*>(dst + jr * D + je + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-        if (je == 0) dst[BM * D + jr] = lse2;
+        for (int e = 0; e < EL; ++e) acc[e] += weight[i] * sums[(i * 16 + jr) * C::ROW + je + e];
+      const float inv = total == 0.f ? 0.f : 1.f / total, lse2 = total == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(total);
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] *= inv;
+      const int at = 16 * n + jr, m = rt * BM + at;
+      if (m < rows) {
+        if (whole) {
+          const int tok = divide(m, p.by_group);
+          store_row<D, EL>(p, static_cast<int64_t>(s.r0 + tok) * p.Hq + head * p.G + (m - tok * p.G), je, acc, lse2);
+        } else {
+          float* const dst = part_of<BM, D>(p, worker, run.x0 > 0);
+#pragma unroll
+          for (int e = 0; e < EL; e += 4) *reinterpret_cast<f32x4*>(dst + at * D + je + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+          if (je == 0) dst[BM * D + at] = lse2;
+        }
       }
     }
     __syncthreads();
@@ -377,27 +418,37 @@ __global__ __launch_bounds__((RowsCfg<D, F8>::NW * 64), (RowsCfg<D, F8>::NW * Ro
   leave_split<BM, BT>(p, worker, split);
 }
 
-constexpr int kMostWorkers = 256 * 8;
+template <int D, bool F8, int NR>
+hipError_t launch_variant(PagedAttn p, hipStream_t stream) {
+  using C = RowsCfg<D, F8, NR>;
+  static_assert(C::PER_CU * (C::LDS + 4 * C::NW * C::LIST) <= 160 * 1024, "");
+  set_workers(p, 256 * C::PER_CU, C::BM, D);
+  const hipError_t e = TASP_LAUNCH((paged_rows_kernel<D, F8, NR>), dim3(static_cast<unsigned>(p.workers)), dim3(C::NW * 64), stream, p);
+  return e != hipSuccess ? e : launch_paged_combine<D, C::BM>(p, stream);
+}
 
 template <int D, bool F8>
-hipError_t launch_variant(PagedAttn p, hipStream_t stream) {
-  using C = RowsCfg<D, F8>;
-  static_assert(256 * C::PER_CU <= kMostWorkers && C::PER_CU * (C::LDS + 4 * C::NW * C::LIST) <= 160 * 1024, "");
-  set_workers(p, 256 * C::PER_CU, C::BM, D);
-  const hipError_t e = TASP_LAUNCH((paged_rows_kernel<D, F8>), dim3(static_cast<unsigned>(p.workers)), dim3(C::NW * 64), stream, p);
-  return e != hipSuccess ? e : launch_paged_combine<D, C::BM>(p, stream);
+hipError_t launch_rows(const PagedAttn& p, int rows, hipStream_t stream) {
+  return rows <= 16 ? launch_variant<D, F8, 1>(p, stream) : launch_variant<D, F8, 2>(p, stream);
+}
+template <int D, bool F8>
+constexpr int64_t workspace_for(int rows) {
+  return rows <= 16 ? workspace_of(256 * RowsCfg<D, F8, 1>::PER_CU, 16, D) : workspace_of(256 * RowsCfg<D, F8, 2>::PER_CU, 32, D);
 }
 
 }  // namespace
 
-int64_t paged_rows_workspace(int d) { return workspace_of(kMostWorkers, 16, d); }
+int64_t paged_rows_workspace(bool e4m3, int d, int rows) {
+  if (d == 64) return e4m3 ? workspace_for<64, true>(rows) : workspace_for<64, false>(rows);
+  return e4m3 ? workspace_for<128, true>(rows) : workspace_for<128, false>(rows);
+}
 
-hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
+hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, int rows, hipStream_t stream) {
   p.tile_cost = kParts / 4;
   p.snap = kParts / 4;
   p.least_share = kParts;
-  if (d == 64) return e4m3 ? launch_variant<64, true>(p, stream) : launch_variant<64, false>(p, stream);
-  return e4m3 ? launch_variant<128, true>(p, stream) : launch_variant<128, false>(p, stream);
+  if (d == 64) return e4m3 ? launch_rows<64, true>(p, rows, stream) : launch_rows<64, false>(p, rows, stream);
+  return e4m3 ? launch_rows<128, true>(p, rows, stream) : launch_rows<128, false>(p, rows, stream);
 }
 
 }  // namespace tasp

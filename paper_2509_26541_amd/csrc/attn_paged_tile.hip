@@ -588,7 +588,7 @@ hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
 
 }  // namespace
 
-int64_t paged_tile_workspace(int d) { return workspace_of(workers_of(false, d), 128, d); }
+int64_t paged_tile_workspace(bool e4m3, int d) { return workspace_of(workers_of(e4m3, d), 128, d); }
 
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
   set_workers(p, workers_of(e4m3, d), 128, d);

@@ -319,11 +319,11 @@ __device__ __forceinline__ float* part_of(const PagedAttn& p, int64_t worker, bo
 // Implemented in cache.hip.
 hipError_t launch_cache_write(const PagedView& c, bool e4m3, const void* k, const void* v, int64_t k_stride, int64_t v_stride, bool fp32, int d, hipStream_t stream);
 hipError_t launch_cache_read(const PagedView& c, bool e4m3, void* k, void* v, bool fp32, int d, hipStream_t stream);
-// Implemented in attn_paged.hip and attn_paged_tile.hip: the kernels for up to 16 rows (token, query head of the group) to a sequence and KV
-// head, and for more; and the bytes of workspace that each takes.
-hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, hipStream_t stream);
-int64_t paged_rows_workspace(int d);
+// Implemented in attn_paged.hip and attn_paged_tile.hip: the kernels for up to 32 rows (token, query head of the group) to a sequence and KV
+// head (`rows`: the most, a hint), and for more; and the bytes of workspace that each takes.
+hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, int rows, hipStream_t stream);
+int64_t paged_rows_workspace(bool e4m3, int d, int rows);
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream);
-int64_t paged_tile_workspace(int d);
+int64_t paged_tile_workspace(bool e4m3, int d);
 
 }  // namespace tasp
