@@ -77,6 +77,7 @@ int check_attn(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_
   p.Hq = a->Hq;
   p.G = a->Hq / c->Hkv;
   if (b->n_rows * p.G > kMost || static_cast<int64_t>(p.G) > kMost || b->n_rows * a->Hq > (int64_t{1} << 36)) return TASP_EUNSUPPORTED_SHAPE;
+  if ((b->n_rows * p.G / 16 + b->n_seqs) * c->Hkv > (int64_t{1} << 26)) return TASP_EUNSUPPORTED_SHAPE;           // row tiles, see set_cut
   const int64_t dense = static_cast<int64_t>(a->Hq) * c->d;
   p.q_stride = a->q_stride == 0 ? dense : a->q_stride;
   if (p.q_stride < dense) return TASP_EINVAL;

@@ -71,11 +71,11 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
   const float c = p.scale_log2e;
   unsigned char* const ring = smem + w * NS * C::STAGE;
 
-  PagedRun<BM, BT, true> run;
+  PagedRun<BM, true> run;
   const int worker = xcd_contiguous(blockIdx.x, p.workers);
   PagedSplit split{0, 0, 0, 0, worker, {0, 0, 0}};
   if (!run.start(p, worker, lane)) {
-    leave_split<BM, BT>(p, worker, split);
+    leave_split(p, worker, split);
     return;
   }
   const unsigned page_bytes = (static_cast<unsigned>(p.c.Hkv) << p.c.ps_log2) * RB;            // (below 2^31, the host sees to it)
@@ -415,14 +415,16 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
     }
     __syncthreads();
   }
-  leave_split<BM, BT>(p, worker, split);
+  leave_split(p, worker, split);
 }
 
 template <int D, bool F8, int NR>
 hipError_t launch_variant(PagedAttn p, hipStream_t stream) {
   using C = RowsCfg<D, F8, NR>;
   static_assert(C::PER_CU * (C::LDS + 4 * C::NW * C::LIST) <= 160 * 1024, "");
-  set_workers(p, 256 * C::PER_CU, C::BM, D);
+  // beside its keys a row tile costs as much as 16 of them, and a run has 64 at least
+  if (!set_cut(p, C::BM, 256 * C::PER_CU, 16, 16, 64)) return hipErrorInvalidValue;
+  place_split(p, C::BM, D);
   const hipError_t e = TASP_LAUNCH((paged_rows_kernel<D, F8, NR>), dim3(static_cast<unsigned>(p.workers)), dim3(C::NW * 64), stream, p);
   return e != hipSuccess ? e : launch_paged_combine<D, C::BM>(p, stream);
 }
@@ -443,10 +445,7 @@ int64_t paged_rows_workspace(bool e4m3, int d, int rows) {
   return e4m3 ? workspace_for<128, true>(rows) : workspace_for<128, false>(rows);
 }
 
-hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, int rows, hipStream_t stream) {
-  p.tile_cost = kParts / 4;
-  p.snap = kParts / 4;
-  p.least_share = kParts;
+hipError_t launch_paged_rows(const PagedAttn& p, bool e4m3, int d, int rows, hipStream_t stream) {
   if (d == 64) return e4m3 ? launch_rows<64, true>(p, rows, stream) : launch_rows<64, false>(p, rows, stream);
   return e4m3 ? launch_rows<128, true>(p, rows, stream) : launch_rows<128, false>(p, rows, stream);
 }

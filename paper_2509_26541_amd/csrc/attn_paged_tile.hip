@@ -64,11 +64,11 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
   const int thread = threadIdx.x, wave_u = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int lane = thread & 63, h = lane >> 5, lq = lane & 31;
   const float c = p.scale_log2e;
-  PagedRun<BM, BT, false> run;
+  PagedRun<BM, false> run;
   const int worker = xcd_contiguous(blockIdx.x, p.workers);
   PagedSplit split{0, 0, 0, 0, worker, {0, 0, 0}};
   if (!run.start(p, worker, lane)) {
-    leave_split<BM, BT>(p, worker, split);
+    leave_split(p, worker, split);
     return;
   }
 
@@ -574,7 +574,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
     run.step();
     more = run.next(p, lane);
   }
-  leave_split<BM, BT>(p, worker, split);
+  leave_split(p, worker, split);
 }
 
 constexpr int workers_of(bool e4m3, int d) { return d == 64 && !e4m3 ? 768 : 512; }       // three and two workgroups to a CU
@@ -591,10 +591,9 @@ hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
 int64_t paged_tile_workspace(bool e4m3, int d) { return workspace_of(workers_of(e4m3, d), 128, d); }
 
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
-  set_workers(p, workers_of(e4m3, d), 128, d);
-  p.tile_cost = 2 * kParts;
-  p.snap = 4 * kParts;
-  p.least_share = 4 * kParts;
+  // beside its keys a row tile costs as much as 128 of them, and less than 256 are not split off one: a partial result is as dear
+  if (!set_cut(p, 128, workers_of(e4m3, d), 128, 256, 256)) return hipErrorInvalidValue;
+  place_split(p, 128, d);
   if (d == 64) return e4m3 ? launch_variant<64, true>(p, stream) : launch_variant<64, false>(p, stream);
   return e4m3 ? launch_variant<128, true>(p, stream) : launch_variant<128, false>(p, stream);
 }

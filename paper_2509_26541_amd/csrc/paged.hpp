@@ -72,8 +72,8 @@ struct PagedAttn {
   int32_t Hq, G, causal, window, sinks, out_fp32;
   float scale_log2e;
   double by_workers;             // 1 / workers
-  int32_t workers;               // workgroups that share the work, and how they do (in parts of a key tile, see PagedCost): what a row
-  int32_t tile_cost, snap, least_share;      // tile costs beside its keys, the least that is split off one, the least that a worker takes
+  int32_t workers;               // workgroups that share the work, and how they do, in parts of 2^key_shift keys (see PagedCost): what a row
+  int32_t key_shift, tile_cost, snap, least_share;      // tile costs beside its keys, the least that is split off one, the least that a worker takes
   Divider by_group;
 };
 
@@ -97,23 +97,24 @@ __host__ __device__ __forceinline__ PagedKeys keys_of(const PagedAttn& p, const 
   return k;
 }
 
-// What the rows of a sequence cost, in parts of a key tile: row tile i of a KV head costs first + i step.  Under the causal mask later
-// row tiles see more keys; with a window all are taken for as long as the longest.  Every row tile costs something: its rows are written.
-constexpr int kParts = 1024;
-struct PagedCost { int row_tiles; int64_t first, step; };
-template <int BM, int BT>
+// What the rows of a sequence cost, in parts of 2^key_shift keys (the host sees to it that all of a call stays below 2^30): row tile i of a KV
+// head costs first + i step.  Under the causal mask later row tiles see more keys; with a window all are taken for as long as the longest.  Every
+// row tile costs something: its rows are written.
+struct PagedCost { int row_tiles, first, step; };
+template <int BM>
 __host__ __device__ __forceinline__ PagedCost cost_of(const PagedAttn& p, const PagedSeq& s) {
   PagedCost c{(s.n * p.G + BM - 1) / BM, 0, 0};
-  int64_t keys = p.causal ? larger(s.kv - s.n, 0) + lesser(s.n, BM / p.G + 1) : s.kv;
-  if (p.causal) c.step = static_cast<int64_t>(kParts) * BM / BT / p.G;
-  if (p.window > 0) {
-    const int64_t most = static_cast<int64_t>(p.window) + BM / p.G + BT + lesser(p.sinks, s.kv);
-    if (keys + static_cast<int64_t>(c.row_tiles) * BM / p.G > most) {
-      keys = lesser<int64_t>(s.kv, most);
+  int keys = s.kv;
+  if (p.causal && s.n <= s.kv) {
+    keys = s.kv - s.n + lesser(s.n, BM / p.G + 1);
+    c.step = (BM >> p.key_shift) / p.G;
+    const int64_t most = static_cast<int64_t>(p.window) + BM / p.G + 64 + lesser(p.sinks, s.kv);
+    if (p.window > 0 && keys + static_cast<int64_t>(s.n) > most) {
+      keys = static_cast<int>(lesser<int64_t>(s.kv, most));
       c.step = 0;
     }
   }
-  c.first = keys * (kParts / BT) + p.tile_cost;
+  c.first = (keys >> p.key_shift) + p.tile_cost;
   // Row tiles that differ little count as equal: where there is one to a worker, no run ends inside.
   if (c.step * c.row_tiles <= c.first / 8) {
     c.first += c.step * c.row_tiles / 2;
@@ -121,56 +122,42 @@ __host__ __device__ __forceinline__ PagedCost cost_of(const PagedAttn& p, const 
   }
   return c;
 }
-// About 1 / x, and a / b rounded down (0 <= a < 2^52, b > 0): the compiler's 64-bit division is some 150 dependent instructions.
-__host__ __device__ __forceinline__ double reciprocal(double x) {
+// All of the first n row tiles.
+__host__ __device__ __forceinline__ int cost_upto(const PagedCost& c, int n) {
+  return n * c.first + (c.step == 0 ? 0 : static_cast<int>(static_cast<int64_t>(n) * (n - 1) / 2 * c.step));
+}
+// The row tile that x parts into a KV head's work fall in (0 <= x < cost_upto(c, row_tiles)).
+__host__ __device__ __forceinline__ int row_tile_at(const PagedCost& c, int x) {
+  if (c.row_tiles <= 1) return 0;
+  if (c.step == 0) return static_cast<int>(static_cast<uint32_t>(x) / static_cast<uint32_t>(c.first));
+  const float b = static_cast<float>(c.first) - 0.5f * static_cast<float>(c.step), s = static_cast<float>(c.step);
+  int i = lesser(larger(static_cast<int>(2.f * static_cast<float>(x) / (b + sqrtf(b * b + 2.f * s * static_cast<float>(x)))), 0), c.row_tiles - 1);
+  while (i > 0 && cost_upto(c, i) > x) --i;
+  while (i + 1 < c.row_tiles && cost_upto(c, i + 1) <= x) ++i;
+  return i;
+}
+// A run that starts or ends x parts into a row tile of cost `cost` does so at a key tile; one that would leave less than `snap` (at least 1) on a
+// side takes or leaves the row tile as a whole.
+__host__ __device__ __forceinline__ int snapped(int x, int cost, int snap) { return x < snap ? 0 : cost - x < snap ? cost : x; }
+__host__ __device__ __forceinline__ double reciprocal(double x) {          // about 1 / x
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_rcp(x);
 #else
   return 1.0 / x;
 #endif
 }
-__host__ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  int64_t q = static_cast<int64_t>(static_cast<double>(a) * reciprocal(static_cast<double>(b)));
-  while (q * b > a) --q;
-  while (a - q * b >= b) ++q;
-  return q;
-}
-// All of the first n row tiles.
-__host__ __device__ __forceinline__ int64_t cost_upto(const PagedCost& c, int64_t n) { return n * c.first + c.step * (n * (n - 1) / 2); }
-// The row tile that x parts into a KV head's work fall in (0 <= x < cost_upto(c, row_tiles)).
-__host__ __device__ __forceinline__ int row_tile_at(const PagedCost& c, int64_t x) {
-  const float b = static_cast<float>(c.first) - 0.5f * static_cast<float>(c.step), s = static_cast<float>(c.step);
-  const float guess = c.step == 0 ? static_cast<float>(x) / b : 2.f * static_cast<float>(x) / (b + sqrtf(b * b + 2.f * s * static_cast<float>(x)));
-  int i = lesser(larger(static_cast<int>(guess), 0), c.row_tiles - 1);
-  while (i > 0 && cost_upto(c, i) > x) --i;
-  while (i + 1 < c.row_tiles && cost_upto(c, i + 1) <= x) ++i;
-  return i;
-}
-// A run that starts or ends x parts into a row tile of cost `cost` does so at a key tile; one that would leave less than `snap` on a side
-// takes or leaves the row tile as a whole.
-__host__ __device__ __forceinline__ int64_t snapped(int64_t x, int64_t cost, int64_t snap) { return x < snap ? 0 : cost - x < snap ? cost : x; }
-__host__ __device__ __forceinline__ int key_tile_at(int64_t x, int64_t cost, int n_tiles) {
+__host__ __device__ __forceinline__ int key_tile_at(int x, int cost, int n_tiles) {
   return x >= cost ? n_tiles : lesser(static_cast<int>(static_cast<double>(x) * reciprocal(static_cast<double>(cost)) * n_tiles), n_tiles);
 }
-
-// A value that all lanes have, in scalar registers.
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32));
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
-__device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), lane);
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+// A worker's share of all work.
+__host__ __device__ __forceinline__ int share_of_all(const PagedAttn& p, int all) {
+  return larger(static_cast<int>(static_cast<double>(all) * p.by_workers) + 1, p.least_share);
 }
 
 // Sums of the lanes up to and with each: lanes of a row of 16 pass theirs on by 1, 2, 4 and 8, then each row's and each half's last lane its own.
 template <int CTRL, int ROWS>
-__device__ __forceinline__ int64_t passed_on(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, ROWS, 0xf, false);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), CTRL, ROWS, 0xf, false);
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
-__device__ __forceinline__ int64_t wave_prefix(int64_t x) {
+__device__ __forceinline__ int passed_on(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_prefix(int x) {
   x += passed_on<0x111, 0xf>(x);
   x += passed_on<0x112, 0xf>(x);
   x += passed_on<0x114, 0xf>(x);
@@ -181,47 +168,33 @@ __device__ __forceinline__ int64_t wave_prefix(int64_t x) {
 }
 
 // 64 sequences, one to a lane, with their work laid end to end: sequence after sequence, KV head after KV head, row tile after row tile.
-template <int BM, int BT>
+template <int BM>
 struct PagedChunk {
   int base;
   PagedSeq s;
   PagedCost c;
-  int64_t head, upto;            // work of a KV head; of this sequence and all before it in this chunk
+  int upto;                      // work of this sequence and all before it in this chunk
   __device__ __forceinline__ void load(const PagedAttn& p, int first, int lane) {
     base = first;
     s = load_seq(p.c, first + lane);
-    c = cost_of<BM, BT>(p, s);
-    head = cost_upto(c, c.row_tiles);
-    upto = wave_prefix(head * p.c.Hkv);
+    c = cost_of<BM>(p, s);
+    upto = wave_prefix(cost_upto(c, c.row_tiles) * p.c.Hkv);
   }
   // work of the chunk's first `i` sequences
-  __device__ __forceinline__ int64_t before(int i) const { return i == 0 ? 0 : of_lane(upto, i - 1); }
+  __device__ __forceinline__ int before(int i) const { return i == 0 ? 0 : __builtin_amdgcn_readlane(upto, i - 1); }
 };
 
-// All work of a call, and how much of it a worker takes.
-template <int BM, int BT>
-__device__ __forceinline__ int64_t share_of(const PagedAttn& p, PagedChunk<BM, BT>& c, int lane) {
-  int64_t all = 0;
-  for (int first = 0; first < p.c.n_seqs; first += 64) {
-    c.load(p, first, lane);
-    all += c.before(64);
-  }
-  if (c.base != 0) c.load(p, 0, lane);
-  return uniform(larger<int64_t>(static_cast<int64_t>(static_cast<double>(all) * p.by_workers) + 1, p.least_share));
-}
-
-// A worker's run of the call's work, one row tile (or piece of one) after the other.  KEEP: the lists of the chunk stay in registers
-// (a dozen of them); otherwise those of a sequence are read again when its turn comes.
-template <int BM, int BT, bool KEEP>
+// A worker's run of the call's work, one row tile (or piece of one) after the other.  KEEP: the lists of the chunk stay in registers;
+// otherwise those of a sequence are read again when its turn comes.
+template <int BM, bool KEEP>
 struct PagedRun {
-  PagedChunk<BM, BT> chunk;
-  int64_t share, from, to;       // the run, in parts from the start of sequence `seq` of the chunk
-  int seq, head, rt;             // the next row tile
+  PagedChunk<BM> chunk;
+  int share, from, to;           // the run, in parts from the start of sequence b
+  int b, seq, head, rt;          // (seq: its place in the chunk) the next row tile
   PagedSeq s;
   PagedCost c;
-  int64_t at, cost;              // where it starts, and its cost
-  int64_t x0, x1;                // what the run has of it
-  int b;
+  int at, cost;                  // where it starts, and its cost
+  int x0, x1;                    // what the run has of it
 
   __device__ __forceinline__ void take(const PagedAttn& p) {
     if constexpr (KEEP) {
@@ -229,41 +202,41 @@ struct PagedRun {
       s.kv = __builtin_amdgcn_readlane(chunk.s.kv, seq);
       s.r0 = __builtin_amdgcn_readlane(chunk.s.r0, seq);
       c.row_tiles = __builtin_amdgcn_readlane(chunk.c.row_tiles, seq);
-      c.first = of_lane(chunk.c.first, seq);
-      c.step = of_lane(chunk.c.step, seq);
-      b = chunk.base + seq;
+      c.first = __builtin_amdgcn_readlane(chunk.c.first, seq);
+      c.step = __builtin_amdgcn_readlane(chunk.c.step, seq);
     } else {
       const PagedSeq one = load_seq(p.c, b);
       s.n = __builtin_amdgcn_readfirstlane(one.n);
       s.kv = __builtin_amdgcn_readfirstlane(one.kv);
       s.r0 = __builtin_amdgcn_readfirstlane(one.r0);
-      c = cost_of<BM, BT>(p, s);
+      c = cost_of<BM>(p, s);
     }
   }
   // false: no work for this worker
   __device__ __forceinline__ bool start(const PagedAttn& p, int worker, int lane) {
-    share = share_of<BM, BT>(p, chunk, lane);
+    int all = 0;
+    for (int first = 0; first < p.c.n_seqs; first += 64) {
+      chunk.load(p, first, lane);
+      all += chunk.before(64);
+    }
+    if (chunk.base != 0) chunk.load(p, 0, lane);
+    share = __builtin_amdgcn_readfirstlane(share_of_all(p, all));
     from = share * worker;
     to = from + share;
+    if (from >= all) return false;
     while (true) {
       const uint64_t behind = __builtin_amdgcn_ballot_w64(chunk.upto > from);
-      if (behind != 0) {
-        seq = __builtin_ctzll(behind);
-        const int64_t before = chunk.before(seq);
-        from -= before;
-        to -= before;
-        break;
-      }
-      const int64_t before = chunk.before(64);
+      seq = behind != 0 ? __builtin_ctzll(behind) : 64;
+      const int before = chunk.before(seq);
       from -= before;
       to -= before;
-      if (chunk.base + 64 >= p.c.n_seqs) return false;
+      if (behind != 0) break;
       chunk.load(p, chunk.base + 64, lane);
     }
     b = chunk.base + seq;
     take(p);
-    const int64_t one = cost_upto(c, c.row_tiles);
-    head = static_cast<int>(quotient(from, one));
+    const int one = cost_upto(c, c.row_tiles);
+    head = static_cast<int>(static_cast<uint32_t>(from) / static_cast<uint32_t>(one));
     rt = row_tile_at(c, from - head * one);
     at = head * one + cost_upto(c, rt);
     return true;
@@ -290,7 +263,7 @@ struct PagedRun {
         continue;
       }
       cost = c.first + rt * c.step;
-      x0 = snapped(larger<int64_t>(from - at, 0), cost, p.snap);
+      x0 = snapped(larger(from - at, 0), cost, p.snap);
       x1 = to - at >= cost ? cost : snapped(to - at, cost, p.snap);
       if (x0 < x1) return true;
       step();
@@ -304,9 +277,23 @@ struct PagedRun {
   __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == cost; }
   // the last worker of a row tile that this one starts, for p.snap <= x1 < cost: runs end at `to` and every `share` behind it
   __device__ __forceinline__ int last_worker(const PagedAttn& p, int worker) const {
-    return worker + 1 + static_cast<int>(quotient(at + cost - p.snap - to, share));
+    return worker + 1 + static_cast<int>(static_cast<uint32_t>(at + cost - p.snap - to) / static_cast<uint32_t>(share));
   }
 };
+
+// The host's part of the cut: workers, and `tile_cost`, `snap` and `least_share` from keys to parts.  False: more work than can be counted.
+inline bool set_cut(PagedAttn& p, int bm, int workers, int tile_cost, int snap, int least_share) {
+  const int64_t tiles = (static_cast<int64_t>(p.c.n_rows) * p.G / bm + p.c.n_seqs) * p.c.Hkv;
+  p.workers = workers;
+  p.by_workers = 1.0 / workers;
+  for (p.key_shift = 0; p.key_shift <= 30; ++p.key_shift) {
+    p.tile_cost = larger(1, tile_cost >> p.key_shift);
+    p.snap = larger(1, snap >> p.key_shift);
+    p.least_share = larger(1, least_share >> p.key_shift);
+    if (tiles * (((static_cast<int64_t>(p.c.cap) + 2 * bm) >> p.key_shift) + 2 + p.tile_cost) < (int64_t{1} << 30)) return true;
+  }
+  return false;
+}
 
 // A partial result: BM rows of d normalised sums, and their log-sum-exps to base 2.  A worker leaves at most two: of the row tile that its run
 // starts in, and of the one that it ends in.
@@ -321,7 +308,7 @@ hipError_t launch_cache_write(const PagedView& c, bool e4m3, const void* k, cons
 hipError_t launch_cache_read(const PagedView& c, bool e4m3, void* k, void* v, bool fp32, int d, hipStream_t stream);
 // Implemented in attn_paged.hip and attn_paged_tile.hip: the kernels for up to 32 rows (token, query head of the group) to a sequence and KV
 // head (`rows`: the most, a hint), and for more; and the bytes of workspace that each takes.
-hipError_t launch_paged_rows(PagedAttn p, bool e4m3, int d, int rows, hipStream_t stream);
+hipError_t launch_paged_rows(const PagedAttn& p, bool e4m3, int d, int rows, hipStream_t stream);
 int64_t paged_rows_workspace(bool e4m3, int d, int rows);
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream);
 int64_t paged_tile_workspace(bool e4m3, int d);

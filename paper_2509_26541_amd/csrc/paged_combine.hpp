@@ -26,7 +26,6 @@ __device__ __forceinline__ void store_row(const PagedAttn& p, int64_t rh, int co
 }
 
 // What every worker leaves in p.split, once, at its end.
-template <int BM, int BT>
 __device__ __forceinline__ void leave_split(const PagedAttn& p, int worker, const PagedSplit& split) {
   if (threadIdx.x == 0) p.split[worker] = split;
 }
@@ -121,10 +120,8 @@ hipError_t launch_paged_combine(const PagedAttn& p, hipStream_t stream) {
 // Bytes of the partial results of `workers` workgroups and of what they leave beside them, and where in a workspace these are.
 constexpr int64_t part_bytes(int workers, int bm, int d) { return (2 * workers * part_floats(bm, d) * 4 + 255) / 256 * 256; }
 constexpr int64_t workspace_of(int workers, int bm, int d) { return part_bytes(workers, bm, d) + workers * static_cast<int64_t>(sizeof(PagedSplit)); }
-inline void set_workers(PagedAttn& p, int workers, int bm, int d) {
-  p.workers = workers;
-  p.by_workers = 1.0 / workers;
-  p.split = reinterpret_cast<PagedSplit*>(reinterpret_cast<unsigned char*>(p.part) + part_bytes(workers, bm, d));
+inline void place_split(PagedAttn& p, int bm, int d) {
+  p.split = reinterpret_cast<PagedSplit*>(reinterpret_cast<unsigned char*>(p.part) + part_bytes(p.workers, bm, d));
 }
 
 }  // namespace

@@ -81,8 +81,9 @@ COMMON = [(dict(k=None), tb.EINVAL), (dict(v=None), tb.EINVAL), (dict(dtype=tb.D
           (dict(dtype=tb.DTYPE_E4M3, v_scale=(4 << 20) + 4), tb.EALIGN), (dict(page_table=None), tb.EINVAL), (dict(kv_len=None), tb.EINVAL), (dict(row_start=None), tb.EINVAL),
           (dict(kv_len=(6 << 20) + 2), tb.EALIGN), (dict(n_seqs=-1), tb.EINVAL), (dict(n_rows=-1), tb.EINVAL), (dict(max_pages=0), tb.EINVAL), (dict(max_rows=-1), tb.EINVAL),
           (dict(max_pages=(1 << 26) + 1), tb.EUNSUPPORTED_SHAPE), (dict(n_rows=(1 << 30) + 1), tb.EUNSUPPORTED_SHAPE), (dict(n_rows=1 << 30), tb.EUNSUPPORTED_SHAPE),
-          (dict(n_seqs=1 << 30), tb.EUNSUPPORTED_SHAPE)]
-ATTN = [(dict(Hq=0), tb.EINVAL), (dict(Hq=3), tb.EINVAL), (dict(mask_mode=tb.MASK_ZIGZAG_CAUSAL), tb.EINVAL), (dict(mask_mode=3), tb.EINVAL), (dict(window=-1), tb.EINVAL),
+          (dict(n_seqs=1 << 30), tb.EUNSUPPORTED_SHAPE), (dict(n_pages=1 << 30, page_size=1024), tb.EUNSUPPORTED_SHAPE),
+          (dict(Hkv=1 << 20, page_size=1024), tb.EUNSUPPORTED_SHAPE)]
+ATTN = [(dict(n_rows=1 << 29, Hq=16), tb.EUNSUPPORTED_SHAPE), (dict(Hq=0), tb.EINVAL), (dict(Hq=3), tb.EINVAL), (dict(mask_mode=tb.MASK_ZIGZAG_CAUSAL), tb.EINVAL), (dict(mask_mode=3), tb.EINVAL), (dict(window=-1), tb.EINVAL),
         (dict(sinks=-1), tb.EINVAL), (dict(mask_mode=tb.MASK_FULL, window=4), tb.EINVAL), (dict(softmax_scale=-1.0), tb.EINVAL), (dict(softmax_scale=math.inf), tb.EINVAL),
         (dict(softmax_scale=math.nan), tb.EINVAL), (dict(out_dtype=tb.DTYPE_E4M3), tb.EUNSUPPORTED_SHAPE), (dict(q_stride=255), tb.EINVAL), (dict(q_stride=260), tb.EALIGN),
         (dict(q=None), tb.EINVAL), (dict(out=None), tb.EINVAL), (dict(lse=None), tb.EINVAL), (dict(q=(8 << 20) + 8), tb.EALIGN), (dict(out=(9 << 20) + 4), tb.EALIGN),
@@ -165,11 +166,11 @@ static void tiles(const PagedAttn& p, const std::vector<int>& seen) {
   for (int b = 0; b < p.c.n_seqs; ++b) {
     const PagedSeq s = load_seq(p.c, b);
     expect(s.r0 >= 0 && s.n >= 0 && s.r0 + s.n <= p.c.n_rows && s.kv >= 0 && s.kv <= p.c.cap, "sequence");
-    const PagedCost c = cost_of<BM, BT>(p, s);
+    const PagedCost c = cost_of<BM>(p, s);
     const int row_tiles = c.row_tiles;
     expect(static_cast<int64_t>(row_tiles) * BM >= static_cast<int64_t>(s.n) * p.G && c.first > 0 && c.step >= 0, "cost");
     for (int i = 0; i < row_tiles; ++i)
-      for (int64_t x : {cost_upto(c, i), cost_upto(c, i) + 1, cost_upto(c, i + 1) - 1}) expect(row_tile_at(c, x) == i, "row tile");
+      for (int x : {cost_upto(c, i), (cost_upto(c, i) + cost_upto(c, i + 1)) / 2, cost_upto(c, i + 1) - 1}) expect(row_tile_at(c, x) == i, "row tile");
     for (int rt = 0; rt < row_tiles; ++rt) {
       const int rows = s.n * p.G, tok0 = rt * BM / p.G, tok1 = (lesser(rt * BM + BM, rows) - 1) / p.G;
       const PagedKeys k = keys_of<BM, BT>(p, s, tok0, tok1);
@@ -202,12 +203,13 @@ static void tiles(const PagedAttn& p, const std::vector<int>& seen) {
 template <int BM, int BT>
 static void runs(const PagedAttn& p) {
   int64_t all = 0;
-  for (int b = 0; b < p.c.n_seqs; ++b) { const PagedCost c = cost_of<BM, BT>(p, load_seq(p.c, b)); all += cost_upto(c, c.row_tiles) * p.c.Hkv; }
-  const int64_t share = larger<int64_t>(static_cast<int64_t>(static_cast<double>(all) * p.by_workers) + 1, p.least_share);
+  for (int b = 0; b < p.c.n_seqs; ++b) { const PagedCost c = cost_of<BM>(p, load_seq(p.c, b)); all += cost_upto(c, c.row_tiles) * p.c.Hkv; }
+  expect(all < (1 << 30), "all");
+  const int64_t share = share_of_all(p, static_cast<int>(all));
   int64_t start = 0;
   for (int b = 0; b < p.c.n_seqs; ++b) {
     const PagedSeq s = load_seq(p.c, b);
-    const PagedCost c = cost_of<BM, BT>(p, s);
+    const PagedCost c = cost_of<BM>(p, s);
     for (int i = 0; i < c.row_tiles * p.c.Hkv; ++i) {
       const int64_t cost = c.first + i % c.row_tiles * c.step;
       const int tiles = rnd() % 50;
@@ -217,14 +219,14 @@ static void runs(const PagedAttn& p) {
       for (int64_t w = larger<int64_t>(start / share - 1, 0); w <= (start + cost) / share; ++w) {
         const int64_t from = w * share, to = from + share;
         if (to <= start || from >= start + cost) continue;
-        const int64_t x0 = snapped(larger<int64_t>(from - start, 0), cost, p.snap), x1 = to - start >= cost ? cost : snapped(to - start, cost, p.snap);
+        const int64_t x0 = snapped(static_cast<int>(larger<int64_t>(from - start, 0)), cost, p.snap), x1 = to - start >= cost ? cost : snapped(static_cast<int>(to - start), cost, p.snap);
         if (x0 >= x1) continue;
         expect(w < p.workers, "worker");
         expect(parts ? w >= first && w <= last && (x0 == 0) == (w == first) : x0 == 0 && x1 == cost, "part");
         expect(key_tile_at(x0, cost, tiles) == upto, "gap");
         upto = key_tile_at(x1, cost, tiles);
         // what the worker that starts a row tile says of the last one
-        if (parts && x0 == 0) expect(w + 1 + quotient(start + cost - p.snap - to, share) == last, "last worker");
+        if (parts && x0 == 0) expect(w + 1 + (start + cost - p.snap - to) / share == last, "last worker");
         ++takers;
       }
       expect(upto == tiles && takers == (parts ? last - first + 1 : 1), "row tile not taken whole");
@@ -245,16 +247,29 @@ int main() {
     p.c.n_pages = 7; p.c.ps_log2 = ps_log2; p.c.Hkv = 2; p.c.n_seqs = n_seqs; p.c.max_pages = max_pages; p.c.n_rows = n_rows; p.c.cap = max_pages << ps_log2;
     p.G = 1 + rnd() % 9; p.tile_cost = 1; p.causal = rnd() % 4 != 0; p.window = p.causal && rnd() % 2 ? 1 + rnd() % 100 : 0; p.sinks = p.window ? rnd() % 70 : 0;
     if (p.window && rnd() % 5 == 0) { p.window = 1 << 30; p.sinks = 2147483647; }
-    p.workers = 1 + rnd() % 300; p.by_workers = 1.0 / p.workers; p.tile_cost = rnd() % 3000; p.snap = 1 + rnd() % 5000; p.least_share = 1 + rnd() % 9000;
-    if (!wild) { runs<16, 128>(p); runs<128, 64>(p); runs<16, 64>(p); }
+    for (int bm : {16, 32, 128}) {
+      expect(set_cut(p, bm, 1 + rnd() % 300, 1 + rnd() % 50, 1 + rnd() % 100, 1 + rnd() % 200), "cut");
+      if (round % 3 == 0) { p.key_shift = rnd() % 4; p.tile_cost = 1 + rnd() % 3; p.snap = 1 + rnd() % 3; }
+      if (!wild && bm == 16) runs<16, 64>(p);
+      if (!wild && bm == 32) runs<32, 64>(p);
+      if (!wild && bm == 128) runs<128, 64>(p);
+    }
     tiles<16, 64>(p, table);
-    tiles<16, 128>(p, table);
+    tiles<32, 64>(p, table);
     tiles<128, 64>(p, table);
     for (int b = 0; b < n_seqs; ++b)
       for (int row = 0; row < n_rows; ++row) {
         const PagedPlace at = place_of(p.c, b, row);
         expect(at.page >= -1 && at.page < p.c.n_pages && at.slot >= 0 && at.slot < (1 << ps_log2), "place");
       }
+  }
+  // the largest batches that are taken keep all work countable
+  for (int i = 0; i < 2000; ++i) {
+    PagedAttn p{};
+    p.c.Hkv = 1 + rnd() % 64; p.G = 1 + rnd() % 64; p.c.cap = 16 << rnd() % 27; p.c.n_seqs = 1 + rnd() % 5000;
+    p.c.n_rows = static_cast<int>(lesser<int64_t>(((int64_t{1} << 26) / p.c.Hkv - p.c.n_seqs) * 16 / p.G, rnd() % (1 << rnd() % 31) + 1));
+    if (p.c.n_rows < 1) continue;
+    for (int bm : {16, 32, 128}) expect(set_cut(p, bm, 512, 128, 256, 256), "not countable");
   }
   return bad != 0;
 }
