@@ -384,10 +384,10 @@ double tasp_chunk_attn_bwd_flops(const tasp_schedule_t* s, const tasp_attn_bwd_a
  *             position kv_len - n + j.
  *   page_table [n_seqs, max_pages]  position t lies in slot t % page_size of page page_table[b][t / page_size].
  *             An entry outside [0, n_pages) names no page: nothing is written there, rows read from there are
- *             0 and its keys are not visible.  Neither are positions below 0.
+ *             0 and its keys are not visible.  So it is with positions below 0 or at and behind max_pages * page_size.
  *   max_rows  the most rows of any sequence, or 0 if it is not known: it decides only which kernel runs.
  * Whatever the lists hold, no access leaves the buffers that the arguments describe: row_start is clipped to
- * [0, n_rows] and kv_len to [0, max_pages * page_size].  Rows of the dense outputs outside
+ * [0, n_rows] and kv_len to at least 0.  Rows of the dense outputs outside
  * [row_start[0], row_start[n_seqs]) are left as they are.  A page may be in several tables (shared
  * prefixes); a position that two rows write in one call holds either, or parts of both.
  * max_pages * page_size <= 2^30, n_rows <= 2^30 (with tasp_paged_attn n_rows * Hq / Hkv <= 2^30).

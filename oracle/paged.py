@@ -75,6 +75,7 @@ def attention(q, k_pages, v_pages, page_table, kv_len, row_start, causal=True, w
         n = row_start[b + 1] - row_start[b]
         for j in range(n):
             t = visible(kv - n + j, kv, causal, window, sinks)
+            t = t[t < len(table) * ps]
             pages = table[t // ps] if len(t) else np.zeros(0, dtype=np.int64)
             t = t[(pages >= 0) & (pages < n_pages)]
             row = row_start[b] + j

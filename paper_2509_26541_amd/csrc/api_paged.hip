@@ -132,7 +132,7 @@ size_t tasp_paged_attn_workspace_bytes(const tasp_paged_cache* c, const tasp_pag
   if (check_attn(c, b, a, &p) != TASP_OK) return 0;
   const int64_t rows = rows_of(p, b);
   const bool e4m3 = c->dtype == TASP_DTYPE_E4M3;
-  return static_cast<size_t>(rows <= kFew ? tasp::paged_rows_workspace(e4m3, c->d, static_cast<int>(rows)) : tasp::paged_tile_workspace(e4m3, c->d));
+  return static_cast<size_t>(rows <= kFew ? tasp::paged_rows_workspace(p, e4m3, c->d, static_cast<int>(rows)) : tasp::paged_tile_workspace(p, e4m3, c->d));
 }
 
 int tasp_paged_attn(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_paged_attn_args* a, void* hip_stream) {

@@ -169,14 +169,14 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
 
     // Zero times an infinity or a NaN would carry V's values to rows that do not see them, and what rounding left of a probability,
     // times an infinity, is NaN for those that do.  Sums that are not finite are formed again, with the rows of V that hold
-    // such values taken out of the product and added one by one.
+    // such values taken out of the product and added one by one; so are those behind very large scores (see beyond_fma).
     auto pass = [&](auto careful) {
       float m_raise[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
 #pragma unroll
         for (int i = 0; i < NDB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        m_run[n] = m_raise[n] = kNegBig;
+        m_run[n] = m_raise[n] = kLeast;
         l_run[n] = l_lo[n] = 0.f;
       }
       if (t0 < t1) {
@@ -255,13 +255,16 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
           // ---- softmax: the running maximum is only raised when it grew by more than 2^8
+          // (careful: m_run is the maximum of the scores themselves, and nothing is rounded before it is taken off)
+          constexpr bool EXACT = decltype(careful)::value;
           const float mx = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])), fmaxf(fmaxf(x[n][4], x[n][5]), fmaxf(x[n][6], x[n][7])));
-          if (__builtin_amdgcn_ballot_w64(mx * c > m_raise[n]) != 0) {
+          if (__builtin_amdgcn_ballot_w64((EXACT ? mx : mx * c) > m_raise[n]) != 0) {
             float m_new = fmaxf(mx, __shfl_xor(mx, 16));
-            m_new = fmaxf(m_run[n], fmaxf(m_new, __shfl_xor(m_new, 32)) * c);
-            const float alpha = fast_exp2(m_run[n] - m_new);
+            m_new = fmaxf(m_new, __shfl_xor(m_new, 32));
+            m_new = fmaxf(m_run[n], EXACT ? m_new : m_new * c);
+            const float alpha = fast_exp2(EXACT ? (m_run[n] - m_new) * c : m_run[n] - m_new);
             m_run[n] = m_new;
-            m_raise[n] = m_new + kRescaleGap;
+            m_raise[n] = EXACT ? m_new : m_new + kRescaleGap;
             l_run[n] *= alpha; l_lo[n] *= alpha;
 #pragma unroll
             for (int i = 0; i < NDB; ++i) o[n][i] *= alpha;
@@ -269,7 +272,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
           float sum = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            x[n][e] = fast_exp2(__builtin_fmaf(x[n][e], c, -m_run[n]));
+            x[n][e] = fast_exp2(EXACT ? (x[n][e] - m_run[n]) * c : __builtin_fmaf(x[n][e], c, -m_run[n]));
             sum += x[n][e];
             if constexpr (F8) x[n][e] *= vs[e];
             hi[n][e] = static_cast<__bf16>(x[n][e]);
@@ -355,6 +358,9 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
         fetch(t + NS, st, soon);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (what was fetched past the end lands in LDS too)
+      if constexpr (decltype(careful)::value)
+#pragma unroll
+        for (int n = 0; n < NR; ++n) m_run[n] = m_run[n] == kLeast ? kLeast : m_run[n] * c;
     };
     pass(std::false_type{});
     {
@@ -365,7 +371,10 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
         for (int i = 0; i < NDB; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) z = __builtin_fmaf(o[n][i][e], 0.f, z);
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(z != 0.f) != 0, 0)) pass(std::true_type{});       // (0 times a number is 0)
+      bool again = z != 0.f;                                     // (0 times a number is 0)
+#pragma unroll
+      for (int n = 0; n < NR; ++n) again |= beyond_fma(m_run[n]);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(again) != 0, 0)) pass(std::true_type{});
     }
 
     // ---- the wavefronts' sums are joined, 16 rows at a time
@@ -383,7 +392,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
       for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(sums + (w * 16 + lq) * C::ROW + 16 * db + 4 * g) = o[n][db];
       if (g == 0) { tops[w * 16 + lq] = m_run[n]; tops[(NW + w) * 16 + lq] = l; }
       __syncthreads();
-      float top = kNegBig, weight[NW], total = 0.f, acc[EL];
+      float top = kLeast, weight[NW], total = 0.f, acc[EL];
 #pragma unroll
       for (int i = 0; i < NW; ++i) top = fmaxf(top, tops[i * 16 + jr]);
 #pragma unroll
@@ -409,7 +418,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
           float* const dst = part_of<BM, D>(p, worker, run.x0 > 0);
 #pragma unroll
           for (int e = 0; e < EL; e += 4) *reinterpret_cast<f32x4*>(dst + at * D + je + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-          if (je == 0) dst[BM * D + at] = lse2;
+          if (je == 0) { dst[BM * D + at] = top; dst[BM * D + BM + at] = total; }
         }
       }
     }
@@ -418,12 +427,15 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
   leave_split(p, worker, split);
 }
 
+// beside its keys a row tile costs as much as 16 of them, and a run has 64 at least
+template <int D, bool F8, int NR>
+bool cut(PagedAttn& p) { return set_cut(p, 16 * NR, 256 * RowsCfg<D, F8, NR>::PER_CU, 16, 16, 64); }
+
 template <int D, bool F8, int NR>
 hipError_t launch_variant(PagedAttn p, hipStream_t stream) {
   using C = RowsCfg<D, F8, NR>;
   static_assert(C::PER_CU * (C::LDS + 4 * C::NW * C::LIST) <= 160 * 1024, "");
-  // beside its keys a row tile costs as much as 16 of them, and a run has 64 at least
-  if (!set_cut(p, C::BM, 256 * C::PER_CU, 16, 16, 64)) return hipErrorInvalidValue;
+  if (!cut<D, F8, NR>(p)) return hipErrorInvalidValue;
   place_split(p, C::BM, D);
   const hipError_t e = TASP_LAUNCH((paged_rows_kernel<D, F8, NR>), dim3(static_cast<unsigned>(p.workers)), dim3(C::NW * 64), stream, p);
   return e != hipSuccess ? e : launch_paged_combine<D, C::BM>(p, stream);
@@ -434,15 +446,16 @@ hipError_t launch_rows(const PagedAttn& p, int rows, hipStream_t stream) {
   return rows <= 16 ? launch_variant<D, F8, 1>(p, stream) : launch_variant<D, F8, 2>(p, stream);
 }
 template <int D, bool F8>
-constexpr int64_t workspace_for(int rows) {
-  return rows <= 16 ? workspace_of(256 * RowsCfg<D, F8, 1>::PER_CU, 16, D) : workspace_of(256 * RowsCfg<D, F8, 2>::PER_CU, 32, D);
+int64_t workspace_for(PagedAttn p, int rows) {
+  if (rows <= 16) return cut<D, F8, 1>(p) ? workspace_of(p, 16, D) : 0;
+  return cut<D, F8, 2>(p) ? workspace_of(p, 32, D) : 0;
 }
 
 }  // namespace
 
-int64_t paged_rows_workspace(bool e4m3, int d, int rows) {
-  if (d == 64) return e4m3 ? workspace_for<64, true>(rows) : workspace_for<64, false>(rows);
-  return e4m3 ? workspace_for<128, true>(rows) : workspace_for<128, false>(rows);
+int64_t paged_rows_workspace(const PagedAttn& p, bool e4m3, int d, int rows) {
+  if (d == 64) return e4m3 ? workspace_for<64, true>(p, rows) : workspace_for<64, false>(p, rows);
+  return e4m3 ? workspace_for<128, true>(p, rows) : workspace_for<128, false>(p, rows);
 }
 
 hipError_t launch_paged_rows(const PagedAttn& p, bool e4m3, int d, int rows, hipStream_t stream) {

@@ -243,7 +243,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
     for (int db = 0; db < NDB; ++db) o[db] = zero16();
     // running max (exp2 domain), this lane's sum in two levels (up to 64 tiles, everything before) and what rounding added to the largest
     // probabilities: as in the kernels of dense K and V
-    float m_run = kNegBig, m_raise = kNegBig, l_run = 0.f, l_lo = 0.f, r_fix = 0.f, mx = kNegBig;
+    float m_run = kLeast, m_raise = kLeast, l_run = 0.f, l_lo = 0.f, r_fix = 0.f, mx = kLeast;
 
     if constexpr (!F8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
@@ -446,14 +446,15 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
       tail(stage0, Sa);
     }
     // ---- Zero times an infinity or a NaN would carry V's values to rows that do not see them.  Where sums are not finite, all are formed again,
-    // a step at a time, with the rows of V that hold such values taken out of the product and added one by one.
+    // a step at a time, with the rows of V that hold such values taken out of the product and added one by one, and with the scores taken off their
+    // maximum as they are (see beyond_fma; m_run is the maximum of the scores themselves here).
     {
       float z = 0.f;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[db][i], 0.f, z);
-      const bool bad = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;       // (0 times a number is 0)
+      const bool bad = __builtin_amdgcn_ballot_w64(z != 0.f || beyond_fma(m_run)) != 0;       // (0 times a number is 0)
       if (lane == 0) odd_waves[wave_u] = bad;
     }
     __syncthreads();                     // everybody has read the last tile, too
@@ -465,7 +466,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
       asm volatile("" : "+v"(th));
       const int ch = th >> 5 & 1, cq = th & 31, cga = th >> 4 & 3, cjj = th & 15, crow = 4 * (cga >> 1) + (cjj >> 2);
       const unsigned c_adr = cq * C::RB + C::swz_k(cq, ch) * 16;
-      m_run = kNegBig; m_raise = kNegBig; l_run = 0.f; l_lo = 0.f; r_fix = 0.f;
+      m_run = kLeast; m_raise = kLeast; l_run = 0.f; l_lo = 0.f; r_fix = 0.f;
       for (int t = 0; t < n_tiles; ++t) {
         if (t % 16 == 0) {
           take_list(t, look_up(t));
@@ -493,14 +494,28 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
         }
         mask(t, t & ~15, Sa);
         static_for<16>([&](auto i) __attribute__((always_inline)) { max_step(i, Sa); });
-        raise();
-        uint64_t hidden = 0;             // of the 32 scores
-        static_for<32>([&](auto ee) __attribute__((always_inline)) {
-          constexpr int E = decltype(ee)::value;
-          hidden |= Sa[E / 16][E % 16] == -__builtin_inff() ? uint64_t{1} << E : 0;
-          exp_one(ee, Sa);
+        const float m_new = fmaxf(m_run, max_of_halves(mx)), alpha = fast_exp2((m_run - m_new) * c);
+        m_run = m_new;
+        l_run *= alpha; l_lo *= alpha; r_fix *= alpha;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) o[db] *= alpha;
+        const float p_top = fast_exp2((mx - m_run) * c);
+        r_fix += static_cast<float>(static_cast<__bf16>(p_top)) - p_top;
+        unsigned hidden = 0;             // of the 32 scores
+        float tile_sum = 0.f;
+        static_for<16>([&](auto ii) __attribute__((always_inline)) {
+          constexpr int I = decltype(ii)::value;
+          float y[2];
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            const float score = Sa[I / 8][2 * I % 16 + f];
+            hidden |= score == -__builtin_inff() ? 1u << (2 * I + f) : 0u;
+            y[f] = fast_exp2((score - m_run) * c);
+            tile_sum += y[f];
+          }
+          pf[I / 4][I % 4] = __builtin_bit_cast(unsigned, bf16x2{static_cast<__bf16>(y[0]), static_cast<__bf16>(y[1])});
         });
-        add_up();
+        l_lo += tile_sum;
         if ((t & 63) == 63) { l_run += l_lo; l_lo = 0.f; }
         __syncthreads();
         for (int j = 0; j < BT; ++j) {
@@ -534,6 +549,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
           }
         __syncthreads();
       }
+      m_run = m_run == kLeast ? kLeast : m_run * c;
     }
     // ---- epilogue
     if (!idle) {
@@ -566,7 +582,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
           for (int db = 0; db < NDB; ++db)
 #pragma unroll
             for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(od + 32 * db + 8 * i) = f32x4{o[db][4 * i] * wb, o[db][4 * i + 1] * wb, o[db][4 * i + 2] * wb, o[db][4 * i + 3] * wb};
-          if (h == 0) part[BM * D + m - rt * BM] = lse2;
+          if (h == 0) { part[BM * D + m - rt * BM] = m_run; part[BM * D + BM + m - rt * BM] = l_tot; }
         }
       }
     }
@@ -577,7 +593,9 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
   leave_split(p, worker, split);
 }
 
-constexpr int workers_of(bool e4m3, int d) { return d == 64 && !e4m3 ? 768 : 512; }       // three and two workgroups to a CU
+// Three and two workgroups to a CU.  Beside its keys a row tile costs as much as 512 of them, and less than 512 are not split off one: a partial result
+// is as dear (12 ragged chunks of up to 1 500 new tokens: 121 us, 137 with 128 and 256; a window of 2 048 at d = 64: 109 and 113).
+bool cut(PagedAttn& p, bool e4m3, int d) { return set_cut(p, 128, d == 64 && !e4m3 ? 768 : 512, 512, 512, 512); }
 
 template <int D, bool F8>
 hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
@@ -588,12 +606,10 @@ hipError_t launch_variant(const PagedAttn& p, hipStream_t stream) {
 
 }  // namespace
 
-int64_t paged_tile_workspace(bool e4m3, int d) { return workspace_of(workers_of(e4m3, d), 128, d); }
+int64_t paged_tile_workspace(PagedAttn p, bool e4m3, int d) { return cut(p, e4m3, d) ? workspace_of(p, 128, d) : 0; }
 
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream) {
-  // beside its keys a row tile costs as much as 512 of them, and less than 512 are not split off one: a partial result is as dear (12 ragged
-  // chunks of up to 1 500 new tokens: 121 us, 137 with 128 and 256; a window of 2 048 at d = 64: 109 and 113)
-  if (!set_cut(p, 128, workers_of(e4m3, d), 512, 512, 512)) return hipErrorInvalidValue;
+  if (!cut(p, e4m3, d)) return hipErrorInvalidValue;
   place_split(p, 128, d);
   if (d == 64) return e4m3 ? launch_variant<64, true>(p, stream) : launch_variant<64, false>(p, stream);
   return e4m3 ? launch_variant<128, true>(p, stream) : launch_variant<128, false>(p, stream);

@@ -28,7 +28,7 @@ __host__ __device__ __forceinline__ constexpr T lesser(T a, T b) { return b < a 
 template <class T>
 __host__ __device__ __forceinline__ constexpr T larger(T a, T b) { return a < b ? b : a; }
 
-// The clipped lists of a sequence: n rows from r0 on, kv tokens.
+// The lists of a sequence, clipped: n rows from r0 on, kv tokens (of which those at and behind p.cap have no page).
 struct PagedSeq { int n, kv, r0; };
 __host__ __device__ __forceinline__ PagedSeq load_seq(const PagedView& p, int i) {
   PagedSeq s{0, 0, 0};
@@ -36,7 +36,7 @@ __host__ __device__ __forceinline__ PagedSeq load_seq(const PagedView& p, int i)
     const int a = p.row_start[i], e = p.row_start[i + 1], len = p.kv_len[i];
     s.r0 = lesser(larger(a, 0), p.n_rows);
     s.n = lesser(larger(e, s.r0), p.n_rows) - s.r0;
-    s.kv = lesser(larger(len, 0), p.cap);
+    s.kv = larger(len, 0);
   }
   return s;
 }
@@ -48,7 +48,7 @@ __host__ __device__ __forceinline__ int page_of(const PagedView& p, int b, int p
 // Where a row of sequence b lives: page and slot, or page -1.
 struct PagedPlace { int page, slot; };
 __host__ __device__ __forceinline__ PagedPlace place_of(const PagedView& p, int b, int64_t row) {
-  const int64_t pos = static_cast<int64_t>(lesser(larger(p.kv_len[b], 0), p.cap)) - p.row_start[b + 1] + row;
+  const int64_t pos = static_cast<int64_t>(larger(p.kv_len[b], 0)) - p.row_start[b + 1] + row;
   if (pos < 0 || pos >= p.cap) return {-1, 0};
   return {page_of(p, b, static_cast<int>(pos)), static_cast<int>(pos) & ((1 << p.ps_log2) - 1)};
 }
@@ -87,7 +87,7 @@ template <int BM, int BT>
 __host__ __device__ __forceinline__ PagedKeys keys_of(const PagedAttn& p, const PagedSeq& s, int tok0, int tok1) {
   PagedKeys k{0, 0, 0, 0};
   const int p0 = s.kv - s.n;
-  k.end = larger(0, p.causal ? p0 + tok1 + 1 : s.kv);
+  k.end = larger(0, lesser(p.causal ? p0 + tok1 + 1 : s.kv, p.c.cap));
   const int last = (k.end + BT - 1) / BT;
   if (p.window > 0) {
     k.from = lesser(larger(0, p0 + tok0 - p.window + 1) / BT, last);
@@ -104,13 +104,14 @@ struct PagedCost { int row_tiles, first, step; };
 template <int BM>
 __host__ __device__ __forceinline__ PagedCost cost_of(const PagedAttn& p, const PagedSeq& s) {
   PagedCost c{(s.n * p.G + BM - 1) / BM, 0, 0};
-  int keys = s.kv;
-  if (p.causal && s.n <= s.kv) {
-    keys = s.kv - s.n + lesser(s.n, BM / p.G + 1);
+  const int kv = lesser(s.kv, p.c.cap);
+  int keys = kv;
+  if (p.causal && s.n <= kv) {
+    keys = kv - s.n + lesser(s.n, BM / p.G + 1);
     c.step = (BM >> p.key_shift) / p.G;
-    const int64_t most = static_cast<int64_t>(p.window) + BM / p.G + 64 + lesser(p.sinks, s.kv);
+    const int64_t most = static_cast<int64_t>(p.window) + BM / p.G + 64 + lesser(p.sinks, kv);
     if (p.window > 0 && keys + static_cast<int64_t>(s.n) > most) {
-      keys = static_cast<int>(lesser<int64_t>(s.kv, most));
+      keys = static_cast<int>(lesser<int64_t>(kv, most));
       c.step = 0;
     }
   }
@@ -174,9 +175,10 @@ struct PagedChunk {
   PagedSeq s;
   PagedCost c;
   int upto;                      // work of this sequence and all before it in this chunk
-  __device__ __forceinline__ void load(const PagedAttn& p, int first, int lane) {
+  __device__ __forceinline__ void load(const PagedAttn& p, int first, int lane) { set(p, first, load_seq(p.c, first + lane)); }
+  __device__ __forceinline__ void set(const PagedAttn& p, int first, const PagedSeq& seq) {
     base = first;
-    s = load_seq(p.c, first + lane);
+    s = seq;
     c = cost_of<BM>(p, s);
     upto = wave_prefix(cost_upto(c, c.row_tiles) * p.c.Hkv);
   }
@@ -214,16 +216,33 @@ struct PagedRun {
   }
   // false: no work for this worker
   __device__ __forceinline__ bool start(const PagedAttn& p, int worker, int lane) {
-    int all = 0;
+    // the sum of all chunks, each one's lists asked for a chunk ahead; lane i keeps the sum of chunk i
+    int all = 0, sums = 0;
+    PagedSeq ahead = load_seq(p.c, lane);
     for (int first = 0; first < p.c.n_seqs; first += 64) {
-      chunk.load(p, first, lane);
-      all += chunk.before(64);
+      const PagedSeq now = ahead;
+      if (first + 64 < p.c.n_seqs) ahead = load_seq(p.c, first + 64 + lane);
+      chunk.set(p, first, now);
+      const int sum = chunk.before(64);
+      sums = lane == first >> 6 ? sum : sums;
+      all += sum;
     }
-    if (chunk.base != 0) chunk.load(p, 0, lane);
     share = __builtin_amdgcn_readfirstlane(share_of_all(p, all));
     from = share * worker;
     to = from + share;
     if (from >= all) return false;
+    if (p.c.n_seqs > 64) {
+      // the chunk: found among the sums, or from the first one on where there are more than 64
+      int k = 0;
+      if (p.c.n_seqs <= 64 * 64) {
+        const int upto = wave_prefix(sums);
+        k = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > from));
+        const int before = k == 0 ? 0 : __builtin_amdgcn_readlane(upto, k - 1);
+        from -= before;
+        to -= before;
+      }
+      chunk.load(p, 64 * k, lane);
+    }
     while (true) {
       const uint64_t behind = __builtin_amdgcn_ballot_w64(chunk.upto > from);
       seq = behind != 0 ? __builtin_ctzll(behind) : 64;
@@ -281,23 +300,26 @@ struct PagedRun {
   }
 };
 
-// The host's part of the cut: workers, and `tile_cost`, `snap` and `least_share` from keys to parts.  False: more work than can be counted.
+// The host's part of the cut: up to `workers` of them, as many as can have work, and `tile_cost`, `snap` and `least_share` from keys to parts.
+// False: more work than can be counted.
 inline bool set_cut(PagedAttn& p, int bm, int workers, int tile_cost, int snap, int least_share) {
   const int64_t tiles = (static_cast<int64_t>(p.c.n_rows) * p.G / bm + p.c.n_seqs) * p.c.Hkv;
-  p.workers = workers;
-  p.by_workers = 1.0 / workers;
+  const int64_t keys = static_cast<int64_t>(p.c.cap) + 2 * bm;
+  p.workers = static_cast<int>(lesser<int64_t>(workers, tiles * (keys + tile_cost) / least_share + 1));
+  p.by_workers = 1.0 / p.workers;
   for (p.key_shift = 0; p.key_shift <= 30; ++p.key_shift) {
     p.tile_cost = larger(1, tile_cost >> p.key_shift);
     p.snap = larger(1, snap >> p.key_shift);
     p.least_share = larger(1, least_share >> p.key_shift);
-    if (tiles * (((static_cast<int64_t>(p.c.cap) + 2 * bm) >> p.key_shift) + 2 + p.tile_cost) < (int64_t{1} << 30)) return true;
+    if (tiles * ((keys >> p.key_shift) + 2 + p.tile_cost) < (int64_t{1} << 30)) return true;
   }
   return false;
 }
 
-// A partial result: BM rows of d normalised sums, and their log-sum-exps to base 2.  A worker leaves at most two: of the row tile that its run
+// A partial result: BM rows of d normalised sums, their maxima (times c, to base 2) and their sums of weights beside those (apart, since the maximum
+// of very large scores would swallow the other's logarithm).  A worker leaves at most two: of the row tile that its run
 // starts in, and of the one that it ends in.
-constexpr int64_t part_floats(int bm, int d) { return static_cast<int64_t>(bm) * (d + 1); }
+constexpr int64_t part_floats(int bm, int d) { return static_cast<int64_t>(bm) * (d + 2); }
 template <int BM, int D>
 __device__ __forceinline__ float* part_of(const PagedAttn& p, int64_t worker, bool starts_inside) {
   return p.part + (2 * worker + (starts_inside ? 0 : 1)) * part_floats(BM, D);
@@ -309,8 +331,8 @@ hipError_t launch_cache_read(const PagedView& c, bool e4m3, void* k, void* v, bo
 // Implemented in attn_paged.hip and attn_paged_tile.hip: the kernels for up to 32 rows (token, query head of the group) to a sequence and KV
 // head (`rows`: the most, a hint), and for more; and the bytes of workspace that each takes.
 hipError_t launch_paged_rows(const PagedAttn& p, bool e4m3, int d, int rows, hipStream_t stream);
-int64_t paged_rows_workspace(bool e4m3, int d, int rows);
+int64_t paged_rows_workspace(const PagedAttn& p, bool e4m3, int d, int rows);
 hipError_t launch_paged_tile(PagedAttn p, bool e4m3, int d, hipStream_t stream);
-int64_t paged_tile_workspace(bool e4m3, int d);
+int64_t paged_tile_workspace(PagedAttn p, bool e4m3, int d);
 
 }  // namespace tasp

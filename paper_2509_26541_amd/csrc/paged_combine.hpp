@@ -9,6 +9,12 @@
 namespace tasp {
 namespace {
 
+constexpr float kLeast = -3.0e38f;       // a running maximum before the first key: below any score that is a number
+
+// Whether a running maximum m = score * c (rounded) is so large that the scores have to be taken off it before they are multiplied: fma(s, c, -m)
+// is off by what rounding took from m, the same for all keys of the row, so that it cancels unless exp2 of it leaves the floats.
+__device__ __forceinline__ bool beyond_fma(float m) { return m != kLeast && __builtin_fabsf(m) > 0x1p29f; }
+
 // EL values from `col` on of the row (token, query head) at index rh, and its log-sum-exp (base 2; -inf: no key).
 template <int D, int EL>
 __device__ __forceinline__ void store_row(const PagedAttn& p, int64_t rh, int col, const float (&x)[EL], float lse2) {
@@ -44,37 +50,38 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
   const int here = min(sp.rows - m0, 16);                       // rows of this workgroup
   const int turns = here > 8 ? 1 : here > 4 ? 2 : here > 2 ? 4 : here > 1 ? 8 : 16, per_turn = 16 / turns;
   const int group = threadIdx.x / 16, je = threadIdx.x % 16 * EL, turn = group / per_turn, jr = first_row + min(group % per_turn, here - 1);
-  float top = -__builtin_inff(), total = 0.f, acc[EL];
+  float top = kLeast, total = 0.f, acc[EL];
 #pragma unroll
   for (int e = 0; e < EL; ++e) acc[e] = 0.f;
   // `N` parts from i0 on, every turns-th of them, all on their way at once
   auto add = [&](auto nn, int i0) __attribute__((always_inline)) {
     constexpr int N = decltype(nn)::value;
-    float l[N];
+    float m[N], l[N];
     f32x4 x[N][EL / 4];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int i = i0 + j * turns;
       const float* const src = part_of<BM, D>(p, i, i != worker);
-      l[j] = src[BM * D + jr];
+      m[j] = src[BM * D + jr];
+      l[j] = src[BM * D + BM + jr];
 #pragma unroll
       for (int e = 0; e < EL / 4; ++e) x[j][e] = *reinterpret_cast<const f32x4*>(src + jr * D + je + 4 * e);
     }
-    float l_new = top;
+    float m_new = top;
 #pragma unroll
-    for (int j = 0; j < N; ++j) l_new = fmaxf(l_new, l[j]);
-    const float a = top == l_new ? 1.f : fast_exp2(top - l_new);
+    for (int j = 0; j < N; ++j) m_new = fmaxf(m_new, m[j]);
+    const float a = fast_exp2(top - m_new);
     total *= a;
 #pragma unroll
     for (int e = 0; e < EL; ++e) acc[e] *= a;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float w = l[j] == -__builtin_inff() ? 0.f : fast_exp2(l[j] - l_new);       // (parts without keys are zeros)
+      const float w = l[j] * fast_exp2(m[j] - m_new);          // (parts without keys are zeros)
       total += w;
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] += x[j][e / 4][e % 4] * w;
     }
-    top = l_new;
+    top = m_new;
   };
   int i = worker + turn;
   for (; i + 7 * turns <= sp.last; i += 8 * turns) add(std::integral_constant<int, 8>{}, i);
@@ -87,20 +94,20 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
     if (je == 0) { tops[group] = top; totals[group] = total; }
     __syncthreads();
     if (turn > 0) return;                                       // (a row tile's last rows)
-    float l_new = top;
-    for (int t = 1; t < turns; ++t) l_new = fmaxf(l_new, tops[t * per_turn + group]);
-    const float a = top == l_new ? 1.f : fast_exp2(top - l_new);
+    float m_new = top;
+    for (int t = 1; t < turns; ++t) m_new = fmaxf(m_new, tops[t * per_turn + group]);
+    const float a = fast_exp2(top - m_new);
     total *= a;
 #pragma unroll
     for (int e = 0; e < EL; ++e) acc[e] *= a;
     for (int t = 1; t < turns; ++t) {
       const int other = t * per_turn + group;
-      const float w = tops[other] == -__builtin_inff() ? (totals[other] == 0.f ? 0.f : totals[other]) : fast_exp2(tops[other] - l_new);
+      const float w = fast_exp2(tops[other] - m_new);
       total += w * totals[other];
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] += w * sums[other][je + e];
     }
-    top = l_new;
+    top = m_new;
   }
   const int m = m0 + group;
   if (group >= here) return;                                    // (so are these)
@@ -108,7 +115,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
 #pragma unroll
   for (int e = 0; e < EL; ++e) acc[e] *= inv;
   const int tok = divide(m, p.by_group);
-  store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, top + __builtin_amdgcn_logf(total));
+  store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, total == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(total));
   }
 }
 
@@ -119,7 +126,7 @@ hipError_t launch_paged_combine(const PagedAttn& p, hipStream_t stream) {
 
 // Bytes of the partial results of `workers` workgroups and of what they leave beside them, and where in a workspace these are.
 constexpr int64_t part_bytes(int workers, int bm, int d) { return (2 * workers * part_floats(bm, d) * 4 + 255) / 256 * 256; }
-constexpr int64_t workspace_of(int workers, int bm, int d) { return part_bytes(workers, bm, d) + workers * static_cast<int64_t>(sizeof(PagedSplit)); }
+inline int64_t workspace_of(const PagedAttn& p, int bm, int d) { return part_bytes(p.workers, bm, d) + p.workers * static_cast<int64_t>(sizeof(PagedSplit)); }
 inline void place_split(PagedAttn& p, int bm, int d) {
   p.split = reinterpret_cast<PagedSplit*>(reinterpret_cast<unsigned char*>(p.part) + part_bytes(p.workers, bm, d));
 }

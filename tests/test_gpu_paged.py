@@ -139,6 +139,56 @@ def test_pages_that_name_none_are_not_visible(tb, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [3, 60])
+def test_a_sequence_that_outgrew_its_table(tb, kind, new):
+    """Tokens behind the table's last page are neither written nor seen, and what is in the pages stays."""
+    page, n_pages, kv = 16, 6, [100, 40]
+    cache, (k, v) = _cache(tb, n_pages, page, 2, 64, kind, 3)
+    table, starts = [[1, 4, 2], [0, 3, 5]], [0, new, 2 * new]
+    before = [x.view(torch.uint8).clone() for x in (cache.k, cache.v)]
+    batch = _batch(tb, table, kv, starts, 2 * new)
+    q = torch.randn((2 * new, 4, 64), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    for args in ((tb.MASK_CAUSAL, 0, 0), (tb.MASK_CAUSAL, 70, 3), (tb.MASK_FULL, 0, 0)):
+        out, lse = tb.tasp_paged_attn(q.cuda(), cache, batch, *args)
+        _check(out, lse, paged.attention(q.double().numpy(), k, v, table, kv, starts, args[0] == tb.MASK_CAUSAL, args[1], args[2]), 64)
+    rows = torch.ones((2 * new, 2, 64), dtype=torch.bfloat16, device="cuda")
+    tb.tasp_cache_write(rows, rows, cache, batch)
+    for x, old in zip((cache.k, cache.v), before):
+        same = (x.view(torch.uint8) == old).all(-1)[:, 0].cpu()                        # [pages, slots]
+        kept = [min(48, kv[b] - new) if kv[b] - new > 0 else 0 for b in range(2)]
+        assert same[table[0]].flatten()[: kept[0]].all() and same[table[1]].flatten()[: kept[1]].all()
+        assert same[table[0]].flatten().sum() == kept[0] and same[table[1]].flatten()[: 40].sum() == kept[1]
+
+
+def test_many_sequences(tb):
+    """More sequences than lanes, and than lanes of lanes: each with one row, a few with none."""
+    for n_seqs in (65, 200, 4200):
+        gen = torch.Generator().manual_seed(n_seqs)
+        kv = torch.randint(0, 40, (n_seqs,), generator=gen).tolist()
+        new = [0 if i % 7 == 3 else 1 for i in range(n_seqs)]
+        starts = np.concatenate([[0], np.cumsum(new)]).tolist()
+        table = torch.randint(0, 50, (n_seqs, 3), generator=gen).tolist()
+        cache, (k, v) = _cache(tb, 50, 16, 1, 64, "bf16", 5)
+        for g in (2, 20):
+            q = torch.randn((starts[-1], g, 64), generator=gen).to(torch.bfloat16)
+            out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, starts, starts[-1], 1 if g == 2 else 8))
+            _check(out, lse, paged.attention(q.double().numpy(), k, v, table, kv, starts), 64)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_scores_far_below_zero(tb, new):
+    kv, page, d = 70, 16, 64
+    k = torch.full((5, 1, page, d), -(2.0**55), dtype=torch.bfloat16, device="cuda")
+    v = torch.randn((5, 1, page, d), device="cuda").to(torch.bfloat16)
+    q = torch.full((new, 2, d), 2.0**60, dtype=torch.bfloat16, device="cuda")
+    table = [[0, 1, 2, 3, 4]]
+    out, lse = tb.tasp_paged_attn(q, tb.PagedCache(k, v), _batch(tb, table, [kv], [0, new], new))
+    want = paged.attention(q.double().cpu().numpy(), k.double().cpu().numpy(), v.double().cpu().numpy(), table, [kv], [0, new])
+    assert np.allclose(lse.double().cpu().numpy(), want[1], rtol=1e-6) and (want[1] < -1e34).all()
+    _check(out, torch.from_numpy(want[1]), (want[0], want[1], want[2], np.zeros_like(want[3])), d)       # (equal scores are equal exactly)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("new", [6, 40])
 def test_what_is_not_seen_does_not_reach_a_row(tb, kind, d, new):
