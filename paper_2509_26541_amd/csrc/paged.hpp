@@ -57,8 +57,8 @@ __host__ __device__ __forceinline__ PagedPlace place_of(const PagedView& p, int 
 __device__ __forceinline__ float scale_value(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // ---- attention: the rows (token, query head of the group) of a sequence and KV head in tiles of BM, their keys in tiles of BT
-// The row tile that a worker's run ends in, if others go on with it: its rows in the dense tensors, and the last of those workers (the
-// worker itself: there is none).
+// The row tile that a worker's run ends in, if others go on with it: where its sequence's rows start in the dense tensors, how many they are
+// (with the query heads of the group), and the last of those workers (the worker itself: there is none).
 struct PagedSplit { int32_t r0, rows, head, rt, last, unused[3]; };
 
 struct PagedAttn {
@@ -267,7 +267,7 @@ struct PagedRun {
         rt = 0;
         ++head;
       }
-      if (head >= p.c.Hkv || c.row_tiles == 0) {
+      if (static_cast<uint32_t>(head) >= static_cast<uint32_t>(p.c.Hkv) || c.row_tiles == 0) {        // (below zero: see last_worker)
         head = rt = 0;
         from -= at;
         to -= at;
@@ -294,9 +294,11 @@ struct PagedRun {
     ++rt;
   }
   __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == cost; }
-  // the last worker of a row tile that this one starts, for p.snap <= x1 < cost: runs end at `to` and every `share` behind it
-  __device__ __forceinline__ int last_worker(const PagedAttn& p, int worker) const {
-    return worker + 1 + static_cast<int>(static_cast<uint32_t>(at + cost - p.snap - to) / static_cast<uint32_t>(share));
+  // the last worker of a row tile that this one starts, for p.snap <= x1 < cost: runs end at `to` and every `share` behind it.  (Lists that fall, so
+  // that sequences share rows, can carry the sum of all work past 32 bits: then the runs end before the row tile does.)
+  __host__ __device__ __forceinline__ int last_worker(const PagedAttn& p, int worker) const {
+    const int more = static_cast<int>(static_cast<uint32_t>(at + cost - p.snap - to) / static_cast<uint32_t>(share));
+    return lesser(worker + 1 + more, p.workers - 1);
   }
 };
 

@@ -497,3 +497,21 @@ def test_two_streams_with_their_own_plans(tb):
     torch.cuda.synchronize()
     for x, p in zip(q, plans):
         _check(p.out, p.lse, paged.attention(x.double().numpy(), k, v, table, [130, 90], [0, 1, 2]), 64)
+
+
+@pytest.mark.parametrize("max_rows", [0, 1])
+def test_lists_that_fall_stay_inside(tb, max_rows):
+    """Sequences that share their rows, against the documented order, with more work than 32 bits count: the call ends, its buffers' surroundings and the
+    cache stay as they were, and so does a row behind the last one."""
+    seqs, rows, page = 300, 2048, 1024
+    cache, _ = _cache(tb, 1, page, 8, 128, "bf16", 5)
+    before = [t.clone() for t in (cache.k, cache.v)]
+    batch = _batch(tb, [[-1] * 64] * seqs, [64 * page] * seqs, [rows * (b % 2) for b in range(seqs + 1)], rows, max_rows)
+    plan = tb.PagedAttnPlan(torch.zeros((rows, 32, 128), dtype=torch.bfloat16, device="cuda"), cache, batch)
+    out, lse = torch.full((rows + 1, 32, 128), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((rows + 1, 32), 7.0, device="cuda")
+    workspace = torch.full((plan.args.workspace_bytes + 65536,), 7, dtype=torch.uint8, device="cuda")
+    plan.args.out, plan.args.lse, plan.args.workspace = out.data_ptr(), lse.data_ptr(), workspace.data_ptr()
+    plan.run()
+    torch.cuda.synchronize()
+    assert (out[rows] == 7).all() and (lse[rows] == 7).all() and (workspace[plan.args.workspace_bytes:] == 7).all()
+    assert torch.equal(before[0], cache.k) and torch.equal(before[1], cache.v)

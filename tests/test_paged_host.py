@@ -271,6 +271,15 @@ int main() {
     if (p.c.n_rows < 1) continue;
     for (int bm : {16, 32, 128}) expect(set_cut(p, bm, 512, 128, 256, 256), "not countable");
   }
+  // lists that fall, so that sequences share rows, can carry the sum of all work past 32 bits: a run's last worker is one of the call's
+  for (int i = 0; i < 2000; ++i) {
+    PagedAttn p{};
+    p.workers = 1 + rnd() % 1000; p.snap = 1 + rnd() % 16;
+    PagedRun<16, true> r{};
+    r.share = 1 + rnd() % 100; r.cost = p.snap + rnd() % 1000000; r.at = rnd() % 1000000; r.to = r.at + rnd() % (r.cost - p.snap + 1);
+    const int worker = rnd() % p.workers, last = r.last_worker(p, worker);
+    expect(last >= worker && last < p.workers, "a worker that is none");
+  }
   return bad != 0;
 }
 """
