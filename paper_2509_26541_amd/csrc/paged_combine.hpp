@@ -45,77 +45,77 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
   const PagedSplit sp = p.split[worker];
   if (sp.last == worker) return;
   for (int first_row = blockIdx.x % PER * ROWS, end_row = first_row + ROWS; first_row < end_row; first_row += 16) {
-  const int m0 = sp.rt * BM + first_row;
-  if (m0 >= sp.rows) return;
-  const int here = min(sp.rows - m0, 16);                       // rows of this workgroup
-  const int turns = here > 8 ? 1 : here > 4 ? 2 : here > 2 ? 4 : here > 1 ? 8 : 16, per_turn = 16 / turns;
-  const int group = threadIdx.x / 16, je = threadIdx.x % 16 * EL, turn = group / per_turn, jr = first_row + min(group % per_turn, here - 1);
-  float top = kLeast, total = 0.f, acc[EL];
+    const int m0 = sp.rt * BM + first_row;
+    if (m0 >= sp.rows) return;
+    const int here = min(sp.rows - m0, 16);                       // rows of this workgroup
+    const int turns = here > 8 ? 1 : here > 4 ? 2 : here > 2 ? 4 : here > 1 ? 8 : 16, per_turn = 16 / turns;
+    const int group = threadIdx.x / 16, je = threadIdx.x % 16 * EL, turn = group / per_turn, jr = first_row + min(group % per_turn, here - 1);
+    float top = kLeast, total = 0.f, acc[EL];
 #pragma unroll
-  for (int e = 0; e < EL; ++e) acc[e] = 0.f;
-  // `N` parts from i0 on, every turns-th of them, all on their way at once
-  auto add = [&](auto nn, int i0) __attribute__((always_inline)) {
-    constexpr int N = decltype(nn)::value;
-    float m[N], l[N];
-    f32x4 x[N][EL / 4];
+    for (int e = 0; e < EL; ++e) acc[e] = 0.f;
+    // `N` parts from i0 on, every turns-th of them, all on their way at once
+    auto add = [&](auto nn, int i0) __attribute__((always_inline)) {
+      constexpr int N = decltype(nn)::value;
+      float m[N], l[N];
+      f32x4 x[N][EL / 4];
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = i0 + j * turns;
-      const float* const src = part_of<BM, D>(p, i, i != worker);
-      m[j] = src[BM * D + jr];
-      l[j] = src[BM * D + BM + jr];
+      for (int j = 0; j < N; ++j) {
+        const int i = i0 + j * turns;
+        const float* const src = part_of<BM, D>(p, i, i != worker);
+        m[j] = src[BM * D + jr];
+        l[j] = src[BM * D + BM + jr];
 #pragma unroll
-      for (int e = 0; e < EL / 4; ++e) x[j][e] = *reinterpret_cast<const f32x4*>(src + jr * D + je + 4 * e);
+        for (int e = 0; e < EL / 4; ++e) x[j][e] = *reinterpret_cast<const f32x4*>(src + jr * D + je + 4 * e);
+      }
+      float m_new = top;
+#pragma unroll
+      for (int j = 0; j < N; ++j) m_new = fmaxf(m_new, m[j]);
+      const float a = fast_exp2(top - m_new);
+      total *= a;
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] *= a;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float w = l[j] * fast_exp2(m[j] - m_new);          // (parts without keys are zeros)
+        total += w;
+#pragma unroll
+        for (int e = 0; e < EL; ++e) acc[e] += x[j][e / 4][e % 4] * w;
+      }
+      top = m_new;
+    };
+    int i = worker + turn;
+    for (; i + 7 * turns <= sp.last; i += 8 * turns) add(std::integral_constant<int, 8>{}, i);
+    if (i + 3 * turns <= sp.last) { add(std::integral_constant<int, 4>{}, i); i += 4 * turns; }
+    for (; i <= sp.last; i += turns) add(std::integral_constant<int, 1>{}, i);
+    if (turns > 1) {                                              // (the same for the whole workgroup)
+      __shared__ float sums[16][D + 4], tops[16], totals[16];
+#pragma unroll
+      for (int e = 0; e < EL; ++e) sums[group][je + e] = acc[e];
+      if (je == 0) { tops[group] = top; totals[group] = total; }
+      __syncthreads();
+      if (turn > 0) return;                                       // (a row tile's last rows)
+      float m_new = top;
+      for (int t = 1; t < turns; ++t) m_new = fmaxf(m_new, tops[t * per_turn + group]);
+      const float a = fast_exp2(top - m_new);
+      total *= a;
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] *= a;
+      for (int t = 1; t < turns; ++t) {
+        const int other = t * per_turn + group;
+        const float w = fast_exp2(tops[other] - m_new);
+        total += w * totals[other];
+#pragma unroll
+        for (int e = 0; e < EL; ++e) acc[e] += w * sums[other][je + e];
+      }
+      top = m_new;
     }
-    float m_new = top;
+    const int m = m0 + group;
+    if (group >= here) return;                                    // (so are these)
+    const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-    for (int j = 0; j < N; ++j) m_new = fmaxf(m_new, m[j]);
-    const float a = fast_exp2(top - m_new);
-    total *= a;
-#pragma unroll
-    for (int e = 0; e < EL; ++e) acc[e] *= a;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float w = l[j] * fast_exp2(m[j] - m_new);          // (parts without keys are zeros)
-      total += w;
-#pragma unroll
-      for (int e = 0; e < EL; ++e) acc[e] += x[j][e / 4][e % 4] * w;
-    }
-    top = m_new;
-  };
-  int i = worker + turn;
-  for (; i + 7 * turns <= sp.last; i += 8 * turns) add(std::integral_constant<int, 8>{}, i);
-  if (i + 3 * turns <= sp.last) { add(std::integral_constant<int, 4>{}, i); i += 4 * turns; }
-  for (; i <= sp.last; i += turns) add(std::integral_constant<int, 1>{}, i);
-  if (turns > 1) {                                              // (the same for the whole workgroup)
-    __shared__ float sums[16][D + 4], tops[16], totals[16];
-#pragma unroll
-    for (int e = 0; e < EL; ++e) sums[group][je + e] = acc[e];
-    if (je == 0) { tops[group] = top; totals[group] = total; }
-    __syncthreads();
-    if (turn > 0) return;                                       // (a row tile's last rows)
-    float m_new = top;
-    for (int t = 1; t < turns; ++t) m_new = fmaxf(m_new, tops[t * per_turn + group]);
-    const float a = fast_exp2(top - m_new);
-    total *= a;
-#pragma unroll
-    for (int e = 0; e < EL; ++e) acc[e] *= a;
-    for (int t = 1; t < turns; ++t) {
-      const int other = t * per_turn + group;
-      const float w = fast_exp2(tops[other] - m_new);
-      total += w * totals[other];
-#pragma unroll
-      for (int e = 0; e < EL; ++e) acc[e] += w * sums[other][je + e];
-    }
-    top = m_new;
-  }
-  const int m = m0 + group;
-  if (group >= here) return;                                    // (so are these)
-  const float inv = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-  for (int e = 0; e < EL; ++e) acc[e] *= inv;
-  const int tok = divide(m, p.by_group);
-  store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, total == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(total));
+    for (int e = 0; e < EL; ++e) acc[e] *= inv;
+    const int tok = divide(m, p.by_group);
+    store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, total == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(total));
   }
 }
 

@@ -34,7 +34,7 @@ def test_direct_loads(asm):
         assert len(loads) >= 8 or "paged_tile_kernelILi64ELb1E" in name or "paged_tile_kernelILi128ELb1E" in name, (name, len(loads))
         for k in loads:
             assert LOAD.fullmatch(ins[k]), (name, ins[k])
-            assert ins[k - 1] == "s_nop 0" and re.match(r"s_mov_b32 m0, s\d+|s_add_u32 m0, s\d+, ", ins[k - 2]), (name, ins[k - 2 : k + 1])
+            assert ins[k - 1] == "s_nop 0" and re.match(r"s_mov_b32 m0, (s\d+|vcc_(lo|hi))$|s_add_u32 m0, s\d+, ", ins[k - 2]), (name, ins[k - 2 : k + 1])
         assert sum("m0" in s for s in ins) == len(loads), name
 
 
