@@ -184,178 +184,176 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
         for (int n = 0; n < NR; ++n)
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) asm volatile("" : "+v"(qf[n][j]));     // (the compiler waits for them here, not in the loop)
+        for (int i = 0; i < NS; ++i) fetch(t0 + i, i, listed_pages(t0 + i));
       }
-      // (the first NS rounds only fetch: in a short call the code itself comes from memory, and this way there is less of it)
-      for (int t = t0 < t1 ? t0 - NS : t1, st = 0; t < t1; ++t, st = st + 1 == NS ? 0 : st + 1) {
+      for (int t = t0, st = 0; t < t1; ++t, st = st + 1 == NS ? 0 : st + 1) {
         const i32x2v soon = listed_pages(t + NS);
-        if (t >= t0) {
-          asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NS - 1) * C::PER_STAGE) : "memory");
-          const unsigned char* const kl = ring + st * C::STAGE;
-          unsigned char* const vl = ring + st * C::STAGE + C::WK * RB;
-          const int pos0 = keys.tile(t) * BT + w * C::WK;
-          const unsigned has = paged >> (2 * (NS - 1)) & 3;
-          // ---- scores: those of keys 4 g .. 4 g + 3 and 16 + 4 g .. of the lane's rows
-          float x[NR][8], vs[8];
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NS - 1) * C::PER_STAGE) : "memory");
+        const unsigned char* const kl = ring + st * C::STAGE;
+        unsigned char* const vl = ring + st * C::STAGE + C::WK * RB;
+        const int pos0 = keys.tile(t) * BT + w * C::WK;
+        const unsigned has = paged >> (2 * (NS - 1)) & 3;
+        // ---- scores: those of keys 4 g .. 4 g + 3 and 16 + 4 g .. of the lane's rows
+        float x[NR][8], vs[8];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            f32x4 sc[NR];
+        for (int i = 0; i < 2; ++i) {
+          f32x4 sc[NR];
 #pragma unroll
-            for (int n = 0; n < NR; ++n) sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const int r = 16 * i + lq;
-            auto product = [&](bf16x8 kf, int j) {
+          for (int n = 0; n < NR; ++n) sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+          const int r = 16 * i + lq;
+          auto product = [&](bf16x8 kf, int j) {
 #pragma unroll
-              for (int n = 0; n < NR; ++n) sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][j], sc[n], 0, 0, 0);
-            };
-            if constexpr (!F8) {
+            for (int n = 0; n < NR; ++n) sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][j], sc[n], 0, 0, 0);
+          };
+          if constexpr (!F8) {
 #pragma unroll
-              for (int j = 0; j < D / 32; ++j) product(*reinterpret_cast<const bf16x8*>(kl + r * RB + ((4 * j + g) ^ C::swz_k(r)) * 16), j);
-            } else {
+            for (int j = 0; j < D / 32; ++j) product(*reinterpret_cast<const bf16x8*>(kl + r * RB + ((4 * j + g) ^ C::swz_k(r)) * 16), j);
+          } else {
 #pragma unroll
-              for (int j = 0; j < D / 64; ++j) {
-                const u32x4 k16 = *reinterpret_cast<const u32x4*>(kl + r * RB + ((4 * j + g) ^ C::swz_k(r)) * 16);
-                product(widen(u32x2{k16[0], k16[1]}), 2 * j);
-                product(widen(u32x2{k16[2], k16[3]}), 2 * j + 1);
-              }
-            }
-            if constexpr (F8) {
-              const unsigned kw = *reinterpret_cast<const unsigned*>(kl + 2 * C::WK * RB + 16 * i + 4 * g);
-              const unsigned vw = *reinterpret_cast<const unsigned*>(kl + 2 * C::WK * RB + 32 + 16 * i + 4 * g);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float ks = scale_value(kw >> 8 * e & 255);
-#pragma unroll
-                for (int n = 0; n < NR; ++n) x[n][4 * i + e] = sc[n][e] * ks;
-                vs[4 * i + e] = scale_value(vw >> 8 * e & 255);
-              }
-            } else {
-#pragma unroll
-              for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[n][4 * i + e] = sc[n][e];
+            for (int j = 0; j < D / 64; ++j) {
+              const u32x4 k16 = *reinterpret_cast<const u32x4*>(kl + r * RB + ((4 * j + g) ^ C::swz_k(r)) * 16);
+              product(widen(u32x2{k16[0], k16[1]}), 2 * j);
+              product(widen(u32x2{k16[2], k16[3]}), 2 * j + 1);
             }
           }
-          unsigned seen[NR];
+          if constexpr (F8) {
+            const unsigned kw = *reinterpret_cast<const unsigned*>(kl + 2 * C::WK * RB + 16 * i + 4 * g);
+            const unsigned vw = *reinterpret_cast<const unsigned*>(kl + 2 * C::WK * RB + 32 + 16 * i + 4 * g);
 #pragma unroll
-          for (int n = 0; n < NR; ++n) seen[n] = 0xff;
-          if (!(has == 3 && pos0 + C::WK - 1 <= all_to && (pos0 >= all_from || pos0 + C::WK <= p.sinks))) {
+            for (int e = 0; e < 4; ++e) {
+              const float ks = scale_value(kw >> 8 * e & 255);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int pos = pos0 + 16 * (e / 4) + 4 * g + e % 4;
-              const bool there = (has >> (e / 4) & 1) != 0 && pos < keys.end;
-#pragma unroll
-              for (int n = 0; n < NR; ++n) {
-                const bool ok = there && pos <= see_to[n] && (pos >= see_from[n] || pos < p.sinks);
-                seen[n] &= ok ? 0xffu : ~(1u << e);
-                x[n][e] = ok ? x[n][e] : -__builtin_inff();
-              }
-              if constexpr (F8) vs[e] = there ? vs[e] : 0.f;       // (a scale behind the end may be anything)
+              for (int n = 0; n < NR; ++n) x[n][4 * i + e] = sc[n][e] * ks;
+              vs[4 * i + e] = scale_value(vw >> 8 * e & 255);
             }
+          } else {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[n][4 * i + e] = sc[n][e];
           }
-          bf16x8 hi[NR], lo[NR];
-#pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            // ---- softmax: the running maximum is only raised when it grew by more than 2^8
-            // (careful: m_run is the maximum of the scores themselves, and nothing is rounded before it is taken off)
-            constexpr bool EXACT = decltype(careful)::value;
-            const float mx = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])), fmaxf(fmaxf(x[n][4], x[n][5]), fmaxf(x[n][6], x[n][7])));
-            if (__builtin_amdgcn_ballot_w64((EXACT ? mx : mx * c) > m_raise[n]) != 0) {
-              float m_new = fmaxf(mx, __shfl_xor(mx, 16));
-              m_new = fmaxf(m_new, __shfl_xor(m_new, 32));
-              m_new = fmaxf(m_run[n], EXACT ? m_new : m_new * c);
-              const float alpha = fast_exp2(EXACT ? (m_run[n] - m_new) * c : m_run[n] - m_new);
-              m_run[n] = m_new;
-              m_raise[n] = EXACT ? m_new : m_new + kRescaleGap;
-              l_run[n] *= alpha; l_lo[n] *= alpha;
-#pragma unroll
-              for (int i = 0; i < NDB; ++i) o[n][i] *= alpha;
-            }
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              x[n][e] = fast_exp2(EXACT ? (x[n][e] - m_run[n]) * c : __builtin_fmaf(x[n][e], c, -m_run[n]));
-              sum += x[n][e];
-              if constexpr (F8) x[n][e] *= vs[e];
-              hi[n][e] = static_cast<__bf16>(x[n][e]);
-              lo[n][e] = static_cast<__bf16>(x[n][e] - static_cast<float>(hi[n][e]));
-            }
-            // in two levels, so that a few large terms do not swallow many small ones
-            l_lo[n] += sum;
-            if ((t & 63) == 63) { l_run[n] += l_lo[n]; l_lo[n] = 0.f; }
-          }
-
-          if constexpr (decltype(careful)::value) {
-            // (places formed here: outside the loop they would take registers from it)
-            int ln = lane;
-            asm volatile("" : "+v"(ln));
-            const int cg = ln >> 4, cq = ln & 15;
-            // rows of V with a value that is not finite: two lanes look at each
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < RB / 32; ++i) {
-              const u32x4 y = *reinterpret_cast<const u32x4*>(vl + ln / 2 * RB + (ln % 2 * (RB / 32) + i) * 16);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if constexpr (F8) {
-#pragma unroll
-                  for (int f = 0; f < 4; ++f) odd |= (y[e] >> 8 * f & 0x7f) == 0x7f;
-                } else {
-                  odd |= (y[e] & 0x7f80u) == 0x7f80u || (y[e] & 0x7f800000u) == 0x7f800000u;
-                }
-              }
-            }
-            uint64_t rows_odd = __builtin_amdgcn_ballot_w64(odd);
-            rows_odd = (rows_odd | rows_odd >> 1) & 0x5555555555555555ull;
-            while (rows_odd != 0) {
-              const int r = __builtin_ctzll(rows_odd) / 2, at_e = r / 16 * 4 + r % 4, from_lane = r % 16 / 4 * 16 + cq;
-              rows_odd &= rows_odd - 1;
-              float pr[NR];
-              bool sees[NR];
-#pragma unroll
-              for (int n = 0; n < NR; ++n) {
-                float mine = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) mine = e == at_e ? x[n][e] : mine;
-                pr[n] = __shfl(mine, from_lane);
-                sees[n] = (__shfl(static_cast<int>(seen[n]), from_lane) >> at_e & 1) != 0;
-              }
-#pragma unroll
-              for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int col = 16 * db + 4 * cg + e;
-                  float y;
-                  if constexpr (F8) {
-                    const unsigned byte = vl[r * RB + (db ^ C::swz_v(r)) * 16 + 4 * cg + e];
-                    y = __builtin_amdgcn_cvt_f32_fp8(byte, 0);
-                  } else {
-                    y = static_cast<float>(*reinterpret_cast<const __bf16*>(vl + r * RB + ((col / 8) ^ C::swz_v(r)) * 16 + col % 8 * 2));
-                  }
-#pragma unroll
-                  for (int n = 0; n < NR; ++n) o[n][db][e] += sees[n] ? pr[n] * y : 0.f;
-                }
-              asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-              if (ln < C::UNITS) *reinterpret_cast<u32x4*>(vl + r * RB + ln * 16) = u32x4{0u, 0u, 0u, 0u};
-              asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            }
-          }
-          // ---- O^T += V^T P^T
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) {
-            bf16x8 vf;
-            if constexpr (!F8) {
-              const int r = 4 * g + (lq >> 2), un = 2 * db + ((lq & 3) >> 1);
-              vf = lds_tr8(vl + r * RB + (un ^ C::swz_v(r)) * 16 + 8 * (lq & 1), vl + (r + 16) * RB + (un ^ C::swz_v(r + 16)) * 16 + 8 * (lq & 1));
-            } else {
-              const int r8 = lq >> 1, r = 4 * g + (r8 & 3) + (r8 >> 2) * 16;
-              vf = widen(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_ptr)(lds_void_ptr)(vl + r * RB + (db ^ C::swz_v(r)) * 16 + 8 * (lq & 1)))));
-            }
-#pragma unroll
-            for (int n = 0; n < NR; ++n) o[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[n], o[n][db], 0, 0, 0);
-#pragma unroll
-            for (int n = 0; n < NR; ++n) o[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[n], o[n][db], 0, 0, 0);
-          }
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the stage has been read
         }
+        unsigned seen[NR];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) seen[n] = 0xff;
+        if (!(has == 3 && pos0 + C::WK - 1 <= all_to && (pos0 >= all_from || pos0 + C::WK <= p.sinks))) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int pos = pos0 + 16 * (e / 4) + 4 * g + e % 4;
+            const bool there = (has >> (e / 4) & 1) != 0 && pos < keys.end;
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              const bool ok = there && pos <= see_to[n] && (pos >= see_from[n] || pos < p.sinks);
+              seen[n] &= ok ? 0xffu : ~(1u << e);
+              x[n][e] = ok ? x[n][e] : -__builtin_inff();
+            }
+            if constexpr (F8) vs[e] = there ? vs[e] : 0.f;       // (a scale behind the end may be anything)
+          }
+        }
+        bf16x8 hi[NR], lo[NR];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          // ---- softmax: the running maximum is only raised when it grew by more than 2^8
+          // (careful: m_run is the maximum of the scores themselves, and nothing is rounded before it is taken off)
+          constexpr bool EXACT = decltype(careful)::value;
+          const float mx = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])), fmaxf(fmaxf(x[n][4], x[n][5]), fmaxf(x[n][6], x[n][7])));
+          if (__builtin_amdgcn_ballot_w64((EXACT ? mx : mx * c) > m_raise[n]) != 0) {
+            float m_new = fmaxf(mx, __shfl_xor(mx, 16));
+            m_new = fmaxf(m_new, __shfl_xor(m_new, 32));
+            m_new = fmaxf(m_run[n], EXACT ? m_new : m_new * c);
+            const float alpha = fast_exp2(EXACT ? (m_run[n] - m_new) * c : m_run[n] - m_new);
+            m_run[n] = m_new;
+            m_raise[n] = EXACT ? m_new : m_new + kRescaleGap;
+            l_run[n] *= alpha; l_lo[n] *= alpha;
+#pragma unroll
+            for (int i = 0; i < NDB; ++i) o[n][i] *= alpha;
+          }
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[n][e] = fast_exp2(EXACT ? (x[n][e] - m_run[n]) * c : __builtin_fmaf(x[n][e], c, -m_run[n]));
+            sum += x[n][e];
+            if constexpr (F8) x[n][e] *= vs[e];
+            hi[n][e] = static_cast<__bf16>(x[n][e]);
+            lo[n][e] = static_cast<__bf16>(x[n][e] - static_cast<float>(hi[n][e]));
+          }
+          // in two levels, so that a few large terms do not swallow many small ones
+          l_lo[n] += sum;
+          if ((t & 63) == 63) { l_run[n] += l_lo[n]; l_lo[n] = 0.f; }
+        }
+
+        if constexpr (decltype(careful)::value) {
+          // (places formed here: outside the loop they would take registers from it)
+          int ln = lane;
+          asm volatile("" : "+v"(ln));
+          const int cg = ln >> 4, cq = ln & 15;
+          // rows of V with a value that is not finite: two lanes look at each
+          bool odd = false;
+#pragma unroll
+          for (int i = 0; i < RB / 32; ++i) {
+            const u32x4 y = *reinterpret_cast<const u32x4*>(vl + ln / 2 * RB + (ln % 2 * (RB / 32) + i) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if constexpr (F8) {
+#pragma unroll
+                for (int f = 0; f < 4; ++f) odd |= (y[e] >> 8 * f & 0x7f) == 0x7f;
+              } else {
+                odd |= (y[e] & 0x7f80u) == 0x7f80u || (y[e] & 0x7f800000u) == 0x7f800000u;
+              }
+            }
+          }
+          uint64_t rows_odd = __builtin_amdgcn_ballot_w64(odd);
+          rows_odd = (rows_odd | rows_odd >> 1) & 0x5555555555555555ull;
+          while (rows_odd != 0) {
+            const int r = __builtin_ctzll(rows_odd) / 2, at_e = r / 16 * 4 + r % 4, from_lane = r % 16 / 4 * 16 + cq;
+            rows_odd &= rows_odd - 1;
+            float pr[NR];
+            bool sees[NR];
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              float mine = 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) mine = e == at_e ? x[n][e] : mine;
+              pr[n] = __shfl(mine, from_lane);
+              sees[n] = (__shfl(static_cast<int>(seen[n]), from_lane) >> at_e & 1) != 0;
+            }
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int col = 16 * db + 4 * cg + e;
+                float y;
+                if constexpr (F8) {
+                  const unsigned byte = vl[r * RB + (db ^ C::swz_v(r)) * 16 + 4 * cg + e];
+                  y = __builtin_amdgcn_cvt_f32_fp8(byte, 0);
+                } else {
+                  y = static_cast<float>(*reinterpret_cast<const __bf16*>(vl + r * RB + ((col / 8) ^ C::swz_v(r)) * 16 + col % 8 * 2));
+                }
+#pragma unroll
+                for (int n = 0; n < NR; ++n) o[n][db][e] += sees[n] ? pr[n] * y : 0.f;
+              }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (ln < C::UNITS) *reinterpret_cast<u32x4*>(vl + r * RB + ln * 16) = u32x4{0u, 0u, 0u, 0u};
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          }
+        }
+        // ---- O^T += V^T P^T
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          bf16x8 vf;
+          if constexpr (!F8) {
+            const int r = 4 * g + (lq >> 2), un = 2 * db + ((lq & 3) >> 1);
+            vf = lds_tr8(vl + r * RB + (un ^ C::swz_v(r)) * 16 + 8 * (lq & 1), vl + (r + 16) * RB + (un ^ C::swz_v(r + 16)) * 16 + 8 * (lq & 1));
+          } else {
+            const int r8 = lq >> 1, r = 4 * g + (r8 & 3) + (r8 >> 2) * 16;
+            vf = widen(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_ptr)(lds_void_ptr)(vl + r * RB + (db ^ C::swz_v(r)) * 16 + 8 * (lq & 1)))));
+          }
+#pragma unroll
+          for (int n = 0; n < NR; ++n) o[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[n], o[n][db], 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) o[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[n], o[n][db], 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the stage has been read
         fetch(t + NS, st, soon);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (what was fetched past the end lands in LDS too)
