@@ -426,11 +426,11 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
   leave_split(p, worker, split);
 }
 
-// Beside its keys a row tile counts as 16 of them, and a run has at least 64.  18 calls of 1 to 512 sequences and 1 to 512 000 tokens, geometric mean:
-// 16, 16, 64 (tile, split, run) 39.0 us; 64, 16, 64 38.4 and 64, 48, 96 38.5 (one token of 700 slower, 12 calls the same); 128, 32, 128 39.4;
-// 192, 64, 256 41.2.
+// Beside its keys a row tile counts as 64 of them; 16 or more are split off one, and a run has at least 64.  18 calls of 1 to 512 sequences and 1 to
+// 512 000 tokens, geometric mean: 64, 16, 64 (tile, split, run) 38.3 us; 16, 16, 64 38.8 (64 sequences of e4m3 203 us for 200); 128, 32, 128 39.1;
+// 192, 64, 256 41.0 (one token of 700: 12.1 for 9.7).
 template <int D, bool F8, int NR>
-bool cut(PagedAttn& p) { return set_cut(p, 16 * NR, 256 * RowsCfg<D, F8, NR>::PER_CU, 16, 16, 64); }
+bool cut(PagedAttn& p) { return set_cut(p, 16 * NR, 256 * RowsCfg<D, F8, NR>::PER_CU, 64, 16, 64); }
 
 template <int D, bool F8, int NR>
 hipError_t launch_variant(PagedAttn p, hipStream_t stream) {
