@@ -3,16 +3,20 @@
 // S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, softmax in one pass (running maximum and sum).  A grouped head's K and V
 // are read once for all 16 rows.  Every wavefront takes keys of its own, in stages of 32, through a part of LDS of its own that loads
 // fill directly: no barrier inside the loop, and the loads run ahead of the products by the stages behind the first.
-// What bounds it is HBM: per key and KV head 4 d bytes (e4m3: 2 d + 2) for 4 d 16 products.
+// What bounds it is HBM: per key and KV head 4 d bytes (e4m3: 2 d + 2) for 4 d 16 products.  One token of 512 000, 8 KV heads of 128: 311 us,
+// 6.6 TB/s of 7.0 that a kernel that only reads gets (e4m3 half of it, 5.9); 64 sequences of e4m3 196 us, 6.1 TB/s.  One token of 700 is latency:
+// 6.6 us, and 2.8 for the joining kernel.
 //
 // The work of a call (sequence after sequence, KV head after KV head, row tile after row tile, in key tiles) is cut into equal runs,
-// one for a workgroup; where a run ends inside a row tile, partial results go to the workspace and paged_rows_combine adds them up,
+// one for a workgroup; where a run ends inside a row tile, partial results go to the workspace and paged_combine_kernel adds them up,
 // always in the same order.  The lengths are on the device, so every workgroup works out its own run.
 //
 // Rounding: P goes into the second product as two bf16 (its value and what rounding that left, 2^-17 of it), which costs a second
 // matrix instruction that HBM hides; everything else is fp32.  e4m3 values are exact in bf16, their scales (powers of two) multiply the
 // scores and the probabilities.
 #include <hip/hip_runtime.h>
+
+#include <climits>
 
 #include "internal.hpp"
 #include "paged.hpp"
