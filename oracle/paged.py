@@ -2,7 +2,7 @@
 
 Row j of sequence b, rows row_start[b] .. row_start[b+1] - 1 of the dense tensors, has position kv_len[b] - n_b + j; position t lies in
 slot t % page_size of page page_table[b][t // page_size].  An entry outside [0, n_pages) names no page: nothing is written there, rows
-read from there are 0, its keys are not visible.
+read from there are 0, its keys are not visible.  row_start counts as at least 0 and at most the number of rows.
 
 e4m3 rows have one factor 2^e: the smallest e >= -100 with max|finite x| <= 448 * 2^e.
 """
@@ -36,9 +36,15 @@ def quantise(x):
     return round_e4m3(x * np.exp2(-exps.astype(np.float64))[..., None]), exps
 
 
-def places(page_table, kv_len, row_start, page_size, n_pages):
-    """[(row, page, slot)] of all rows; page None where there is none."""
+def clipped(row_start, n_rows):
+    """row_start as it counts for tensors of n_rows rows."""
+    return [min(max(int(x), 0), n_rows) for x in row_start]
+
+
+def places(page_table, kv_len, row_start, page_size, n_pages, n_rows=None):
+    """[(row, page, slot)] of all rows; page None where there is none.  n_rows: rows of the dense tensors (by default the list's last entry)."""
     got = []
+    row_start = clipped(row_start, row_start[-1] if n_rows is None else n_rows)
     for b, kv in enumerate(kv_len):
         for row in range(row_start[b], row_start[b + 1]):
             pos = kv - row_start[b + 1] + row
@@ -67,6 +73,7 @@ def attention(q, k_pages, v_pages, page_table, kv_len, row_start, causal=True, w
     q, k_pages, v_pages = (np.asarray(x, dtype=np.float64) for x in (q, k_pages, v_pages))
     rows, hq, d = q.shape
     n_pages, hkv, ps, _ = k_pages.shape
+    row_start = clipped(row_start, rows)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     out, size = np.full((rows, hq, d), np.nan), np.full((rows, hq, d), np.nan)
     lse, reach = np.full((rows, hq), np.nan), np.zeros((rows, hq))

@@ -45,10 +45,11 @@ __host__ __device__ __forceinline__ int page_of(const PagedView& p, int b, int p
   const int page = p.table[static_cast<int64_t>(b) * p.max_pages + (pos >> p.ps_log2)];
   return page >= 0 && page < p.n_pages ? page : -1;
 }
-// Where a row of sequence b lives: page and slot, or page -1.
+// Where a row of sequence b lives: page and slot, or page -1.  (The sequence's last row is the one that load_seq gives it: a list that reaches
+// beyond the rows ends with them.)
 struct PagedPlace { int page, slot; };
 __host__ __device__ __forceinline__ PagedPlace place_of(const PagedView& p, int b, int64_t row) {
-  const int64_t pos = static_cast<int64_t>(larger(p.kv_len[b], 0)) - p.row_start[b + 1] + row;
+  const int64_t pos = static_cast<int64_t>(larger(p.kv_len[b], 0)) - lesser(p.row_start[b + 1], p.n_rows) + row;
   if (pos < 0 || pos >= p.cap) return {-1, 0};
   return {page_of(p, b, static_cast<int>(pos)), static_cast<int>(pos) & ((1 << p.ps_log2) - 1)};
 }

@@ -1,0 +1,50 @@
+"""The paged cache on the GPU at the far ends of what its arguments may hold, against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+from tests.test_gpu_paged import _batch, _cache, _check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tb():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    from paper_2509_26541_amd import binding
+    return binding
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("starts", [[0, 20], [0, 5, 30], [2, 9, 12, 40]])
+def test_lists_that_reach_beyond_the_rows(tb, kind, starts):
+    """row_start counts as at most n_rows, for the write, the read and the attention alike: the last sequence has fewer rows, and they are its last ones."""
+    page, hkv, hq, d, n_rows = 16, 2, 4, 64, 12
+    kv = [60, 45, 100][: len(starts) - 1]
+    table = [[7 * b + i for i in range(7)] for b in range(len(kv))]
+    cache, (k, v) = _cache(tb, 21, page, hkv, d, kind, 4)
+    gen = torch.Generator().manual_seed(8)
+    rows = [torch.randn((n_rows, hkv, d), generator=gen).to(torch.bfloat16) for _ in range(2)]
+    before = [x.view(torch.uint8).cpu() for x in (cache.k, cache.v)]
+    batch = _batch(tb, table, kv, starts, n_rows)
+    tb.tasp_cache_write(rows[0].cuda(), rows[1].cuda(), cache, batch)
+    changed = torch.zeros((21, page), dtype=torch.bool)
+    for row, p, slot in paged.places(table, kv, starts, page, 21, n_rows):
+        changed[p, slot] = True
+        for x, values in zip(rows, (k, v)):
+            y = x[row].double().numpy()
+            if kind == "e4m3":
+                y, exps = paged.quantise(y)
+                y = y * np.exp2(exps.astype(np.float64))[:, None]
+            values[p, :, slot] = y
+    for x, old in zip((cache.k, cache.v), before):
+        assert torch.equal((x.view(torch.uint8).cpu() != old).any(-1).any(1), changed)
+    plan = tb.CacheReadPlan(cache, batch, torch.float32)
+    for x, values in zip(plan.run(), (k, v)):
+        for row, p, slot in paged.places(table, kv, starts, page, 21, n_rows):
+            assert np.array_equal(x[row].double().cpu().numpy(), values[p, :, slot])
+    q = torch.randn((n_rows, hq, d), generator=gen).to(torch.bfloat16)
+    for hint in (1, 40):                                       # both kernels
+        out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, starts, n_rows, hint))
+        _check(out, lse, paged.attention(q.double().numpy(), k, v, table, kv, starts), d)
