@@ -39,7 +39,7 @@ struct RowsCfg {
   static constexpr int STAGE = 2 * WK * RB + (F8 ? 256 : 0), PER_STAGE = 2 * LOADS + (F8 ? 1 : 0);
   static constexpr int LIST = 256;                       // pages a wavefront looks up at once, one for every 16 keys
   static constexpr int ROW = D + 4;                      // floats of a row of sums while they are joined
-  static constexpr int RING = NW * NS * STAGE, JOIN = NW * 16 * ROW * 4 + NW * 16 * 8, LDS = RING > JOIN ? RING : JOIN;
+  static constexpr int RING = NW * NS * STAGE, JOIN = NW * 16 * ROW * 4 + NW * 16 * 12, LDS = RING > JOIN ? RING : JOIN;
   static constexpr int NDB = D / 16;
   // 16-byte units of a stage's row are kept at unit ^ swz: the 16 rows that one read takes a unit (K) or two (V) of then lie in different banks
   __device__ static int swz_k(int r) { return (r / (16 / UNITS)) % UNITS; }
@@ -108,7 +108,9 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
       for (int j = 0; j < D / 32; ++j) qf[n][j] = *reinterpret_cast<const bf16x8*>(src + (F8 ? 64 * (j / 2) + 16 * g + 8 * (j % 2) : 32 * j + 8 * g));
     }
     f32x4 o[NR][NDB];
-    float m_run[NR], l_run[NR], l_lo[NR];
+    float m_run[NR], l_run[NR], l_lo[NR], m_rest[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) m_rest[n] = 0.f;
 
     // (what the loads and the loop go by is the same in all lanes, and said to be)
     const int t0 = scalar(key_tile_at(run.x0, run.cost, keys.n_tiles)), t1 = scalar(key_tile_at(run.x1, run.cost, keys.n_tiles));
@@ -363,7 +365,12 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (what was fetched past the end lands in LDS too)
       if constexpr (decltype(careful)::value)
 #pragma unroll
-        for (int n = 0; n < NR; ++n) m_run[n] = m_run[n] == kLeast ? kLeast : m_run[n] * c;
+        for (int n = 0; n < NR; ++n) {
+          const float m = m_run[n];
+          if (m == kLeast) continue;
+          m_run[n] = m * c;
+          m_rest[n] = rest_of_product(m, c, m_run[n]);
+        }
     };
     pass(std::false_type{});
     {
@@ -382,7 +389,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
 
     // ---- the wavefronts' sums are joined, 16 rows at a time
     float* const sums = reinterpret_cast<float*>(smem);
-    float* const tops = sums + NW * 16 * C::ROW;
+    float* const tops = sums + NW * 16 * C::ROW;                 // references, their rests, sums of weights
     constexpr int TPR = NW * 64 / 16, EL = D / TPR;              // threads to a row, and its values to each
     const int jr = thread / TPR, je = thread % TPR * EL;
 #pragma unroll
@@ -393,15 +400,19 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
       __syncthreads();
 #pragma unroll
       for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(sums + (w * 16 + lq) * C::ROW + 16 * db + 4 * g) = o[n][db];
-      if (g == 0) { tops[w * 16 + lq] = m_run[n]; tops[(NW + w) * 16 + lq] = l; }
+      if (g == 0) { tops[w * 16 + lq] = m_run[n]; tops[(NW + w) * 16 + lq] = m_rest[n]; tops[(2 * NW + w) * 16 + lq] = l; }
       __syncthreads();
-      float top = kLeast, weight[NW], total = 0.f, acc[EL];
-#pragma unroll
-      for (int i = 0; i < NW; ++i) top = fmaxf(top, tops[i * 16 + jr]);
+      Reference m[NW], top{kLeast, 0.f};
+      float weight[NW], total = 0.f, acc[EL];
 #pragma unroll
       for (int i = 0; i < NW; ++i) {
-        weight[i] = fast_exp2(tops[i * 16 + jr] - top);
-        total += weight[i] * tops[(NW + i) * 16 + jr];
+        m[i] = Reference{tops[i * 16 + jr], tops[(NW + i) * 16 + jr]};
+        top = top.larger_of(m[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        weight[i] = fast_exp2(m[i].less(top));
+        total += weight[i] * tops[(2 * NW + i) * 16 + jr];
       }
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] = 0.f;
@@ -409,19 +420,19 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
       for (int i = 0; i < NW; ++i)
 #pragma unroll
         for (int e = 0; e < EL; ++e) acc[e] += weight[i] * sums[(i * 16 + jr) * C::ROW + je + e];
-      const float inv = total == 0.f ? 0.f : 1.f / total, lse2 = total == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(total);
+      const float inv = total == 0.f ? 0.f : 1.f / total, lse2 = total == 0.f ? -__builtin_inff() : top.m + (top.rest + __builtin_amdgcn_logf(total));
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] *= inv;
-      const int at = 16 * n + jr, m = rt * BM + at;
-      if (m < rows) {
+      const int at = 16 * n + jr, row = rt * BM + at;
+      if (row < rows) {
         if (whole) {
-          const int tok = divide(m, p.by_group);
-          store_row<D, EL>(p, static_cast<int64_t>(s.r0 + tok) * p.Hq + head * p.G + (m - tok * p.G), je, acc, lse2);
+          const int tok = divide(row, p.by_group);
+          store_row<D, EL>(p, static_cast<int64_t>(s.r0 + tok) * p.Hq + head * p.G + (row - tok * p.G), je, acc, lse2);
         } else {
           float* const dst = part_of<BM, D>(p, worker, run.x0 > 0);
 #pragma unroll
           for (int e = 0; e < EL; e += 4) *reinterpret_cast<f32x4*>(dst + at * D + je + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-          if (je == 0) { dst[BM * D + at] = top; dst[BM * D + BM + at] = total; }
+          if (je == 0) { dst[BM * D + at] = top.m; dst[BM * D + BM + at] = total; dst[BM * D + 2 * BM + at] = top.rest; }
         }
       }
     }

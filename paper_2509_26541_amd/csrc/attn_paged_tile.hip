@@ -458,6 +458,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
       const bool bad = __builtin_amdgcn_ballot_w64(z != 0.f || beyond_fma(m_run)) != 0;       // (0 times a number is 0)
       if (lane == 0) odd_waves[wave_u] = bad;
     }
+    float m_rest = 0.f;
     __syncthreads();                     // everybody has read the last tile, too
     if (__builtin_expect((odd_waves[0] | odd_waves[1] | odd_waves[2] | odd_waves[3]) != 0, 0)) {
 #pragma unroll
@@ -550,14 +551,18 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
           }
         __syncthreads();
       }
-      m_run = m_run == kLeast ? kLeast : m_run * c;
+      if (m_run != kLeast) {
+        const float m = m_run;
+        m_run = m * c;
+        m_rest = rest_of_product(m, c, m_run);
+      }
     }
     // ---- epilogue
     if (!idle) {
       const float l_mine = l_run + l_lo;
       const float l_tot = l_mine + __shfl_xor(l_mine, 32), r_tot = l_tot + (r_fix + __shfl_xor(r_fix, 32));
       const bool none = l_tot == 0.f;
-      const float wb = none ? 0.f : 1.f / r_tot, lse2 = none ? -__builtin_inff() : m_run + __builtin_amdgcn_logf(l_tot);
+      const float wb = none ? 0.f : 1.f / r_tot, lse2 = none ? -__builtin_inff() : m_run + (m_rest + __builtin_amdgcn_logf(l_tot));
       if (m < rows) {
         if (whole) {
           const int64_t rh = static_cast<int64_t>(run.s.r0 + tok) * p.Hq + head * p.G + mc - tok * p.G;
@@ -583,7 +588,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
           for (int db = 0; db < NDB; ++db)
 #pragma unroll
             for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(od + 32 * db + 8 * i) = f32x4{o[db][4 * i] * wb, o[db][4 * i + 1] * wb, o[db][4 * i + 2] * wb, o[db][4 * i + 3] * wb};
-          if (h == 0) { part[BM * D + m - rt * BM] = m_run; part[BM * D + BM + m - rt * BM] = l_tot; }
+          if (h == 0) { float* const beside = part + BM * D + m - rt * BM; beside[0] = m_run; beside[BM] = l_tot; beside[2 * BM] = m_rest; }
         }
       }
     }

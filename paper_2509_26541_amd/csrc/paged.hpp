@@ -319,10 +319,10 @@ inline bool set_cut(PagedAttn& p, int bm, int workers, int tile_cost, int snap, 
   return false;
 }
 
-// A partial result: BM rows of d normalised sums, their maxima (times c, to base 2) and their sums of weights beside those (apart, since the maximum
-// of very large scores would swallow the other's logarithm).  A worker leaves at most two: of the row tile that its run
-// starts in, and of the one that it ends in.
-constexpr int64_t part_floats(int bm, int d) { return static_cast<int64_t>(bm) * (d + 2); }
+// A partial result: BM rows of d normalised sums, their maxima (times c, to base 2), their sums of weights beside those (apart, since the maximum
+// of very large scores would swallow the other's logarithm) and what rounding took from the maxima (see rest_of_product).  A worker leaves at most
+// two: of the row tile that its run starts in, and of the one that it ends in.
+constexpr int64_t part_floats(int bm, int d) { return static_cast<int64_t>(bm) * (d + 3); }
 template <int BM, int D>
 __device__ __forceinline__ float* part_of(const PagedAttn& p, int64_t worker, bool starts_inside) {
   return p.part + (2 * worker + (starts_inside ? 0 : 1)) * part_floats(BM, D);

@@ -48,3 +48,25 @@ def test_lists_that_reach_beyond_the_rows(tb, kind, starts):
     for hint in (1, 40):                                       # both kernels
         out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, starts, n_rows, hint))
         _check(out, lse, paged.attention(q.double().numpy(), k, v, table, kv, starts), d)
+
+
+@pytest.mark.parametrize("hint", [1, 64])
+@pytest.mark.parametrize("kv,low,high", [(64, 5, 40), (64, 40, 5), (2000, 5, 1900), (9000, 8900, 100), (9000, 100, 8900)])
+def test_large_scores_that_differ(tb, kv, low, high, hint):
+    """Scores 3 2^31 + 1 024 and + 1 536 (times 1/8), exact in fp32: they differ by 64, though their products with log2(e) round to the same float.  The keys lie
+    with two wavefronts, or with two workgroups; the larger one takes all the weight."""
+    page, d, hq = 64, 64, 2
+    c = np.float32(1.4426950408889634) / np.float32(8)
+    assert np.float32(3 * 2**31 + 1024) * c == np.float32(3 * 2**31 + 1536) * c
+    n = -(-kv // page)
+    k = torch.zeros((n, 1, page, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.randn((n, 1, page, d), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    for t, x in ((low, 32.0), (high, 48.0)):
+        k[t // page, 0, t % page, 0], k[t // page, 0, t % page, 1] = 1.5 * 2.0**16, x
+    q = torch.zeros((1, hq, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0], q[..., 1] = 2.0**16, 32.0
+    table = [list(range(n))]
+    out, lse = tb.tasp_paged_attn(q, tb.PagedCache(k, v), _batch(tb, table, [kv], [0, 1], 1, hint), out_dtype=torch.float32)
+    want = v[high // page, 0, high % page].float()
+    assert (out[0] - want).abs().max() <= 2.0**-20 * want.abs().max()                  # the other key's weight is 2^-92
+    assert ((lse.double() - (3 * 2.0**31 + 1536) / 8).abs() <= 2.0**-22 * 2.0**30).all()
