@@ -1,4 +1,6 @@
 """The paged cache on the GPU at the far ends of what its arguments may hold, against the oracle in 64 bits."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -70,3 +72,40 @@ def test_large_scores_that_differ(tb, kv, low, high, hint):
     want = v[high // page, 0, high % page].float()
     assert (out[0] - want).abs().max() <= 2.0**-20 * want.abs().max()                  # the other key's weight is 2^-92
     assert ((lse.double() - (3 * 2.0**31 + 1536) / 8).abs() <= 2.0**-22 * 2.0**30).all()
+
+
+@pytest.mark.parametrize("hint", [1, 64])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scale_bytes_from_0_to_26(tb, d, hint):
+    """Factors that the write never makes.  Byte 0 stands for 0 and the others for 2^(b - 127): read back exactly where the type holds the product; what they
+    add to an output is right to 2^-110 (64 keys, each off by at most 2^-134 times 448)."""
+    page, n_pages = 16, 4
+    gen = torch.Generator().manual_seed(6)
+    x = torch.randn((2, n_pages, 1, page, d), generator=gen).clamp(-4, 4).mul(64).to(torch.float8_e4m3fn)
+    for name in ("zero", "small"):
+        byte = torch.zeros((n_pages, 1, page), dtype=torch.uint8) if name == "zero" else torch.randint(0, 27, (n_pages, 1, page), generator=gen).to(torch.uint8)
+        factor = torch.where(byte == 0, 0.0, torch.exp2(byte.double() - 127))[..., None]
+        cache = tb.PagedCache(x[0].cuda(), x[1].cuda(), *(byte.view(torch.float8_e8m0fnu).cuda() for _ in range(2)))
+        table, kv = [[2, 0, 3, 1]], [64]
+        batch = _batch(tb, table, kv, [0, 64], 64, 64)
+        for dtype in (torch.float32, torch.bfloat16):
+            for got, pages in zip(tb.tasp_cache_read(cache, batch, dtype), x):
+                want = (pages.double() * factor)[table[0]].transpose(1, 2).reshape(64, 1, d)
+                assert torch.equal(got.double().cpu(), want.to(dtype).double())
+        q = torch.randn((1, 3, d), generator=gen).to(torch.bfloat16)
+        out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, [0, 1], 1, hint), out_dtype=torch.float32)
+        want = paged.attention(q.double().numpy(), (x[0].double() * factor).numpy(), (x[1].double() * factor).numpy(), table, kv, [0, 1])
+        assert np.abs(lse.double().cpu().numpy() - math.log(64)).max() <= 2.0**-20
+        err = np.abs(out.double().cpu().numpy() - want[0])
+        assert (err <= (0 if name == "zero" else 2.0**-110 + 2.0**-6 * want[2])).all(), float(err.max())
+        # the same bytes for K alone: scores of 0, ordinary values
+        cache = tb.PagedCache(x[0].cuda(), x[1].cuda(), byte.view(torch.float8_e8m0fnu).cuda(), torch.full_like(byte, 121).view(torch.float8_e8m0fnu).cuda())
+        out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, [0, 1], 1, hint))
+        _check(out, lse, paged.attention(q.double().numpy(), (x[0].double() * factor).numpy(), (x[1].double() / 64).numpy(), table, kv, [0, 1]), d)
+        # 0 times NaN is NaN, in its column alone
+        if name == "zero":
+            pages = x[1].clone()
+            pages.view(torch.uint8)[3, 0, 7, 11] = 0x7F
+            cache = tb.PagedCache(x[0].cuda(), pages.cuda(), *(byte.view(torch.float8_e8m0fnu).cuda() for _ in range(2)))
+            out, _ = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, [0, 1], 1, hint))
+            assert torch.isnan(out[..., 11]).all() and not out[..., [i for i in range(d) if i != 11]].any()
