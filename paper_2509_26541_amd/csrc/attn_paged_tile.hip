@@ -295,7 +295,8 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
     };
     auto v_fragment = [&](auto ff) __attribute__((always_inline)) { constexpr int F = decltype(ff)::value % PD; return u32x4{fl[F][0], fl[F][1], fh[F][0], fh[F][1]}; };
     static_assert(NF % PD == 0 && NF % 2 == 0 && NV % 2 == 0 && PD % 2 == 0 && 4 * C::TILE_BYTES <= 65536, "");
-    auto mask = [&](int t, int listed, f32x16 (&S)[2]) __attribute__((always_inline)) {
+    // hide(kb, i) for every score of a tile that its row does not see
+    auto for_hidden = [&](int t, int listed, auto hide) __attribute__((always_inline)) {
       if (__builtin_expect(is_easy(t, listed), 1)) return;
       const unsigned has = static_cast<unsigned>(paged >> ((t - listed) * 4)) & 15;
       const int at0 = keys.tile(t0 + t) * BT + 4 * h;
@@ -304,8 +305,11 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int pos = at0 + 32 * kb + 8 * (i / 4) + i % 4;
-          if (!((has >> (2 * kb + i / 8) & 1) != 0 && pos <= see_to && (pos >= see_from || pos < p.sinks))) S[kb][i] = -__builtin_inff();
+          if (!((has >> (2 * kb + i / 8) & 1) != 0 && pos <= see_to && (pos >= see_from || pos < p.sinks))) hide(kb, i);
         }
+    };
+    auto mask = [&](int t, int listed, f32x16 (&S)[2]) __attribute__((always_inline)) {
+      for_hidden(t, listed, [&](int kb, int i) __attribute__((always_inline)) { S[kb][i] = -__builtin_inff(); });
     };
     auto max_step = [&](auto ii, f32x16 (&S)[2]) __attribute__((always_inline)) {      // scores 2 I, 2 I + 1 of the 32 a lane holds
       constexpr int I = decltype(ii)::value;
@@ -502,7 +506,8 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
           for (int j = 0; j < NJ; ++j)
             Sa[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(smem + kb * 32 * C::RB + (c_adr ^ (32 * j))), __builtin_bit_cast(bf16x8, qf[j]), Sa[kb], 0, 0, 0);
         }
-        mask(t, t & ~15, Sa);
+        unsigned hidden = 0;             // of the 32 scores (a score that is seen can be -inf, too)
+        for_hidden(t, t & ~15, [&](int kb, int i) __attribute__((always_inline)) { Sa[kb][i] = -__builtin_inff(); hidden |= 1u << (16 * kb + i); });
         static_for<16>([&](auto i) __attribute__((always_inline)) { max_step(i, Sa); });
         const float m_new = fmaxf(m_run, max_of_halves(mx)), alpha = fast_exp2((m_run - m_new) * c);
         m_run = m_new;
@@ -511,16 +516,13 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
         for (int db = 0; db < NDB; ++db) o[db] *= alpha;
         const float p_top = fast_exp2((mx - m_run) * c);
         r_fix += static_cast<float>(static_cast<__bf16>(p_top)) - p_top;
-        unsigned hidden = 0;             // of the 32 scores
         float tile_sum = 0.f;
         static_for<16>([&](auto ii) __attribute__((always_inline)) {
           constexpr int I = decltype(ii)::value;
           float y[2];
 #pragma unroll
           for (int f = 0; f < 2; ++f) {
-            const float score = Sa[I / 8][2 * I % 16 + f];
-            hidden |= score == -__builtin_inff() ? 1u << (2 * I + f) : 0u;
-            y[f] = fast_exp2((score - m_run) * c);
+            y[f] = fast_exp2((Sa[I / 8][2 * I % 16 + f] - m_run) * c);
             tile_sum += y[f];
           }
           pf[I / 4][I % 4] = __builtin_bit_cast(unsigned, bf16x2{static_cast<__bf16>(y[0]), static_cast<__bf16>(y[1])});

@@ -109,3 +109,25 @@ def test_scale_bytes_from_0_to_26(tb, d, hint):
             cache = tb.PagedCache(x[0].cuda(), pages.cuda(), *(byte.view(torch.float8_e8m0fnu).cuda() for _ in range(2)))
             out, _ = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, [0, 1], 1, hint))
             assert torch.isnan(out[..., 11]).all() and not out[..., [i for i in range(d) if i != 11]].any()
+
+
+@pytest.mark.parametrize("hint", [1, 64])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_score_of_minus_infinity_is_seen(tb, d, hint):
+    """A key of -inf has weight 0 for rows with a positive product, and 0 times an infinite value is NaN, as in the formula; a row behind which the key lies
+    has neither."""
+    page, new, kv, at = 16, 3, 40, 38
+    cache, (k, v) = _cache(tb, 3, page, 1, d, "bf16", 4)
+    for pages, host, x in ((cache.k, k, -math.inf), (cache.v, v, math.inf)):
+        pages[at // page, 0, at % page, 9] = x
+        host[at // page, 0, at % page, 9] = x
+    q = torch.randn((new, 2, d), generator=torch.Generator().manual_seed(5)).abs().to(torch.bfloat16)
+    out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, [[0, 1, 2]], [kv], [0, new], new, hint))
+    want = paged.attention(q.double().numpy(), k, v, [[0, 1, 2]], [kv], [0, new])
+    assert np.isnan(want[0][1:, :, 9]).all() and np.isfinite(want[0][0]).all() and np.isfinite(want[1]).all()
+    assert torch.isnan(out[1:, :, 9]).all()
+    rest = [i for i in range(d) if i != 9]
+    reach = np.where(np.isfinite(want[3]), want[3], 32.0)
+    size = np.where(np.isfinite(want[2]), want[2], 4.0)
+    _check(out[..., rest], lse, (want[0][..., rest], want[1], size[..., rest], reach), d)
+    _check(out[:1], lse[:1], tuple(x[:1] for x in want), d)
