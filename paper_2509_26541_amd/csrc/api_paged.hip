@@ -83,7 +83,7 @@ int check_attn(const tasp_paged_cache* c, const tasp_paged_batch* b, const tasp_
   if (p.q_stride < dense) return TASP_EINVAL;
   if (p.q_stride % 8 != 0) return TASP_EALIGN;
   p.causal = a->mask_mode == TASP_MASK_CAUSAL;
-  p.window = a->window < kMost ? a->window : static_cast<int32_t>(kMost);      // (no position is as far)
+  p.window = a->window;
   p.sinks = a->window > 0 ? a->sinks : 0;
   p.out_fp32 = a->out_dtype == TASP_DTYPE_FP32;
   p.scale_log2e = (a->softmax_scale == 0.f ? 1.f / std::sqrt(static_cast<float>(c->d)) : a->softmax_scale) * tasp::kLog2e;

@@ -95,14 +95,14 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
     const int tok0 = divide(rt * BM, p.by_group), tok1 = divide(min(rt * BM + BM, rows) - 1, p.by_group);
     PagedKeys keys = keys_of<BM, BT>(p, s, tok0, tok1);
     const int p0 = s.kv - s.n;
-    const int all_to = min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1), all_from = p.window > 0 ? p0 + tok1 - p.window + 1 : INT_MIN;
+    const int all_to = min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1), all_from = p.window > 0 ? window_start(p0 + tok1, p.window) : INT_MIN;
     int see_to[NR], see_from[NR];                  // the lane's rows see keys up to the one, from the other on or among the first
     bf16x8 qf[NR][D / 32];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const int m = min(rt * BM + 16 * n + lq, rows - 1), tok = divide(m, p.by_group);
       see_to[n] = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1);
-      see_from[n] = p.window > 0 ? p0 + tok - p.window + 1 : INT_MIN;
+      see_from[n] = p.window > 0 ? window_start(p0 + tok, p.window) : INT_MIN;
       const __bf16* const src = static_cast<const __bf16*>(p.q) + static_cast<int64_t>(s.r0 + tok) * p.q_stride + static_cast<int64_t>(head * p.G + m - tok * p.G) * D;
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) qf[n][j] = *reinterpret_cast<const bf16x8*>(src + (F8 ? 64 * (j / 2) + 16 * g + 8 * (j % 2) : 32 * j + 8 * g));

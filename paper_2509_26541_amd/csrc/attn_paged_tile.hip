@@ -111,8 +111,8 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
     const int tok0 = divide(rt * BM, p.by_group), tok1 = divide(min(rt * BM + BM, rows) - 1, p.by_group);
     PagedKeys keys = keys_of<BM, BT>(p, run.s, tok0, tok1);
     const int p0 = run.s.kv - run.s.n;
-    const int see_to = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1), see_from = p.window > 0 ? p0 + tok - p.window + 1 : INT_MIN;
-    const int all_to = scalar(min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1)), all_from = scalar(p.window > 0 ? p0 + tok1 - p.window + 1 : INT_MIN);
+    const int see_to = min(p.causal ? p0 + tok : INT_MAX, keys.end - 1), see_from = p.window > 0 ? window_start(p0 + tok, p.window) : INT_MIN;
+    const int all_to = scalar(min(p.causal ? p0 + tok0 : INT_MAX, keys.end - 1)), all_from = scalar(p.window > 0 ? window_start(p0 + tok1, p.window) : INT_MIN);
     // (what the loader and the loop go by is the same in all lanes, and said to be)
     const int t0 = scalar(key_tile_at(run.x0, run.cost, keys.n_tiles)), n_tiles = scalar(key_tile_at(run.x1, run.cost, keys.n_tiles)) - t0;
     keys.n_first = scalar(keys.n_first);

@@ -84,6 +84,8 @@ struct PagedKeys {
   int n_first, from, n_tiles, end;
   __host__ __device__ __forceinline__ int tile(int u) const { return u < n_first ? u : u - n_first + from; }
 };
+// The first key of the window of a row at `pos` (a key below 0 is none; pos, window and what comes of them are in 32 bits).
+__host__ __device__ __forceinline__ int window_start(int pos, int window) { return larger(pos + 1, 0) - window; }
 template <int BM, int BT>
 __host__ __device__ __forceinline__ PagedKeys keys_of(const PagedAttn& p, const PagedSeq& s, int tok0, int tok1) {
   PagedKeys k{0, 0, 0, 0};
@@ -91,7 +93,7 @@ __host__ __device__ __forceinline__ PagedKeys keys_of(const PagedAttn& p, const 
   k.end = larger(0, lesser(p.causal ? p0 + tok1 + 1 : s.kv, p.c.cap));
   const int last = (k.end + BT - 1) / BT;
   if (p.window > 0) {
-    k.from = lesser(larger(0, p0 + tok0 - p.window + 1) / BT, last);
+    k.from = lesser(larger(0, window_start(p0 + tok0, p.window)) / BT, last);
     k.n_first = lesser((lesser(p.sinks, k.end) + BT - 1) / BT, k.from);
   }
   k.n_tiles = k.n_first + last - k.from;

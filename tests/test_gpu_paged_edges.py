@@ -131,3 +131,29 @@ def test_a_score_of_minus_infinity_is_seen(tb, d, hint):
     size = np.where(np.isfinite(want[2]), want[2], 4.0)
     _check(out[..., rest], lse, (want[0][..., rest], want[1], size[..., rest], reach), d)
     _check(out[:1], lse[:1], tuple(x[:1] for x in want), d)
+
+
+@pytest.mark.parametrize("hint", [1, 64])
+@pytest.mark.parametrize("window", [2**30, 2**30 + 7, 2**31 - 1])
+def test_windows_and_lengths_near_2_31(tb, window, hint):
+    """Sequences that have outgrown their table by far: what a wide window still reaches of the pages is seen."""
+    page, d, new = 16, 64, 3
+    cache, (k, v) = _cache(tb, 4, page, 1, d, "bf16", 9)
+    q = torch.randn((2 * new, 2, d), generator=torch.Generator().manual_seed(5)).to(torch.bfloat16)
+    kv = [min(window + 23, 2**31 - 1), min(window + 40, 2**31 - 1)]
+    table, starts = [[0, 1, 2, 3], [3, 1, 0, 2]], [0, new, 2 * new]
+    out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, starts, 2 * new, hint), tb.MASK_CAUSAL, window, 2)
+    want = [np.full((2 * new, 2, d), np.nan), np.full((2 * new, 2), np.nan), np.full((2 * new, 2, d), np.nan), np.zeros((2 * new, 2))]
+    for b in range(2):
+        for j in range(new):
+            pos = kv[b] - new + j
+            seen = [t for t in range(4 * page) if t > pos - window or t < 2]
+            # one row at a time: the oracle, without a mask, over the keys that it sees
+            kk, vv = (np.stack([x[p, :, s] for p, s in ((table[b][t // page], t % page) for t in seen)]) for x in (k, v))
+            row = starts[b] + j
+            pad = -len(kk) % page
+            as_pages = lambda x: np.concatenate([x, np.zeros((pad, 1, d))]).reshape(-1, page, 1, d).transpose(0, 2, 1, 3)  # noqa: E731
+            got = paged.attention(q[row : row + 1].double().numpy(), as_pages(kk), as_pages(vv), [list(range((len(kk) + pad) // page))], [len(kk)], [0, 1], causal=False)
+            for dst, src in zip(want, got):
+                dst[row] = src[0]
+    _check(out, lse, want, d)

@@ -70,6 +70,42 @@ def test_rows_are_written_where_they_attend_from(tmp_path):
     _run(tmp_path, PLACES)
 
 
+WINDOWS = r"""
+int main() {
+  for (int round = 0; round < 4000; ++round) {
+    int table[8] = {0, 1, 2, 3, 0, 1, 2, 3}, start[2] = {0, 1 + static_cast<int>(rnd() % 40)}, kv = 2147483647 - static_cast<int>(rnd() % 100);
+    PagedAttn p{};
+    p.window = 2147483647 - static_cast<int>(rnd() % 150);
+    if (round % 3 == 1) { p.window = (1 << 30) + static_cast<int>(rnd() % 100); kv = p.window + static_cast<int>(rnd() % 100); }
+    if (round % 3 == 2) kv = static_cast<int>(rnd() % 60);                  // fewer tokens than rows, too
+    p.c.table = table; p.c.kv_len = &kv; p.c.row_start = start;
+    p.c.n_pages = 4; p.c.ps_log2 = 4; p.c.Hkv = 1; p.c.n_seqs = 1; p.c.max_pages = 8; p.c.n_rows = start[1]; p.c.cap = 128;
+    p.G = 1 + rnd() % 3; p.tile_cost = 1; p.causal = 1; p.sinks = rnd() % 20;
+    const PagedSeq s = load_seq(p.c, 0);
+    for (int rt = 0; rt * 16 < s.n * p.G; ++rt) {
+      const int tok0 = rt * 16 / p.G, tok1 = (lesser(rt * 16 + 16, s.n * p.G) - 1) / p.G;
+      const PagedKeys k = keys_of<16, 64>(p, s, tok0, tok1);
+      for (int tok = tok0; tok <= tok1; ++tok)
+        for (int t = 0; t < lesser(s.kv, 128); ++t) {
+          const int64_t pos = static_cast<int64_t>(s.kv) - s.n + tok;
+          const bool seen = t <= pos && (t > pos - p.window || t < p.sinks);
+          expect(seen == (t <= pos && (t >= window_start(s.kv - s.n + tok, p.window) || t < p.sinks)), "the mask of a row");
+          bool in = false;
+          for (int u = 0; u < k.n_tiles && !in; ++u) in = t / 64 == k.tile(u);
+          expect(!seen || (in && t < k.end), "a key that is seen is in no tile");
+        }
+    }
+  }
+  return bad != 0;
+}
+"""
+
+
+@needs_hipcc
+def test_windows_and_lengths_near_2_31_stay_in_32_bits(tmp_path):
+    _run(tmp_path, WINDOWS)
+
+
 def test_the_oracle_clips_its_lists():
     rng = np.random.default_rng(3)
     table, kv = [[0, 1, 2], [3, 4, 5]], [40, 30]
