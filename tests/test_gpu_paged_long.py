@@ -1,4 +1,4 @@
-"""Attention over a paged cache where every workgroup walks many key tiles, against 64 bits.
+"""Attention over a paged cache where every workgroup walks many key tiles, and the precision of the kernel for few rows, against 64 bits.
 
 Tolerances.  With reach = scale max sum |q k| and size = sum p |v|: a score is off by (d + 4) 2^-24 reach.  Its exponential is taken by
 the hardware (2^-22) of an argument that lies within 2^5 of 0 wherever the weight counts (rounded: 2^-20), so a probability is off by
@@ -13,7 +13,7 @@ import pytest
 import torch
 
 from tests import paged_shapes
-from tests.test_gpu_paged import _batch, _cache
+from tests.test_gpu_paged import _batch, _cache, _table
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,28 @@ def test_long_runs(tb, kind, d, tokens, windowed):
             plan.out.fill_(7.0)
             again, lse_again = plan.run()
             assert torch.equal(again.view(torch.int32), out.view(torch.int32)) and torch.equal(lse_again, lse)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq,hkv,d,new", [(4, 4, 128, 1), (16, 2, 128, 2), (8, 1, 64, 4), (6, 2, 64, 3)])
+def test_few_rows_keep_probabilities_to_17_bits(tb, kind, hq, hkv, d, new):
+    """fp32 outputs of up to 32 rows over up to 64 keys, of which each of two wavefronts has one stage; the bound is one that P in one bf16 does not keep."""
+    kv, page = [64, 3, 33, 17, 50, 64, 7, 5], 16
+    starts = [new * i for i in range(len(kv) + 1)]
+    kv = [max(x, new) for x in kv]
+    cache, (k, v) = _cache(tb, 40, page, hkv, d, kind, 23)
+    table = _table(kv, page, 40, 2)
+    q = (torch.randn((starts[-1], hq, d), generator=torch.Generator().manual_seed(5)) / 4).to(torch.bfloat16)
+    out, lse = tb.tasp_paged_attn(q.cuda(), cache, _batch(tb, table, kv, starts, starts[-1], new), out_dtype=torch.float32)
+    want = _exact(q.double(), torch.from_numpy(k), torch.from_numpy(v), table, kv, starts)
+    bounds = _bounds(want, d, 1, True)
+    coarse = torch.full_like(want[0], np.nan)                  # P rounded to bf16, everything else exact
+    for b in range(len(kv)):
+        for row in range(starts[b], starts[b + 1]):
+            t = np.arange(kv[b] - new + row - starts[b] + 1)
+            for h in range(hq):
+                at = (np.asarray(table[b])[t // page], h * hkv // hq, t % page)
+                s = torch.from_numpy(k[at]) @ q[row, h].double() / d**0.5
+                coarse[row, h] = torch.exp(s - s.max()).to(torch.bfloat16).double() @ torch.from_numpy(v[at]) / torch.exp(s - s.max()).sum()
+    assert float(((coarse - want[0]).abs() / bounds[0]).max()) > 4
+    _compare(out.cpu(), lse.cpu(), want, bounds)
