@@ -366,10 +366,11 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
       if constexpr (decltype(careful)::value)
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-          const float m = m_run[n];
-          if (m == kLeast) continue;
-          m_run[n] = m * c;
-          m_rest[n] = rest_of_product(m, c, m_run[n]);
+          float times;
+          m_rest[n] = rest_of_product(m_run[n], c, times);
+          l_run[n] *= times; l_lo[n] *= times;
+#pragma unroll
+          for (int i = 0; i < NDB; ++i) o[n][i] *= times;
         }
     };
     pass(std::false_type{});
@@ -402,25 +403,32 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
       for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(sums + (w * 16 + lq) * C::ROW + 16 * db + 4 * g) = o[n][db];
       if (g == 0) { tops[w * 16 + lq] = m_run[n]; tops[(NW + w) * 16 + lq] = m_rest[n]; tops[(2 * NW + w) * 16 + lq] = l; }
       __syncthreads();
-      Reference m[NW], top{kLeast, 0.f};
-      float weight[NW], total = 0.f, acc[EL];
+      float top = kLeast, top_rest = 0.f, weight[NW], total = 0.f, acc[EL];
 #pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        m[i] = Reference{tops[i * 16 + jr], tops[(NW + i) * 16 + jr]};
-        top = top.larger_of(m[i]);
+      for (int i = 0; i < NW; ++i) top = fmaxf(top, tops[i * 16 + jr]);
+#pragma unroll
+      for (int i = 0; i < NW; ++i) weight[i] = fast_exp2(tops[i * 16 + jr] - top);
+      if (__builtin_expect(beyond_fma(top), 0)) {
+        top = tops[jr]; top_rest = tops[NW * 16 + jr];
+#pragma unroll
+        for (int i = 1; i < NW; ++i) {
+          const float m = tops[i * 16 + jr], rest = tops[(NW + i) * 16 + jr];
+          const bool more = less(m, rest, top, top_rest) > 0.f;
+          top = more ? m : top;
+          top_rest = more ? rest : top_rest;
+        }
+#pragma unroll
+        for (int i = 0; i < NW; ++i) weight[i] = fast_exp2(less(tops[i * 16 + jr], tops[(NW + i) * 16 + jr], top, top_rest));
       }
 #pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        weight[i] = fast_exp2(m[i].less(top));
-        total += weight[i] * tops[(2 * NW + i) * 16 + jr];
-      }
+      for (int i = 0; i < NW; ++i) total += weight[i] * tops[(2 * NW + i) * 16 + jr];
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] = 0.f;
 #pragma unroll
       for (int i = 0; i < NW; ++i)
 #pragma unroll
         for (int e = 0; e < EL; ++e) acc[e] += weight[i] * sums[(i * 16 + jr) * C::ROW + je + e];
-      const float inv = total == 0.f ? 0.f : 1.f / total, lse2 = total == 0.f ? -__builtin_inff() : top.m + (top.rest + __builtin_amdgcn_logf(total));
+      const float inv = total == 0.f ? 0.f : 1.f / total, lse2 = total == 0.f ? -__builtin_inff() : top + (top_rest + __builtin_amdgcn_logf(total));
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] *= inv;
       const int at = 16 * n + jr, row = rt * BM + at;
@@ -432,7 +440,7 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
           float* const dst = part_of<BM, D>(p, worker, run.x0 > 0);
 #pragma unroll
           for (int e = 0; e < EL; e += 4) *reinterpret_cast<f32x4*>(dst + at * D + je + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-          if (je == 0) { dst[BM * D + at] = top.m; dst[BM * D + BM + at] = total; dst[BM * D + 2 * BM + at] = top.rest; }
+          if (je == 0) { dst[BM * D + at] = top; dst[BM * D + BM + at] = total; dst[BM * D + 2 * BM + at] = top_rest; }
         }
       }
     }

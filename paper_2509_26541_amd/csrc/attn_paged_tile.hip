@@ -561,11 +561,11 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
           }
         __syncthreads();
       }
-      if (m_run != kLeast) {
-        const float m = m_run;
-        m_run = m * c;
-        m_rest = rest_of_product(m, c, m_run);
-      }
+      float times;
+      m_rest = rest_of_product(m_run, c, times);
+      l_run *= times; l_lo *= times; r_fix *= times;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[db] *= times;
     }
     // ---- epilogue
     if (!idle) {

@@ -322,7 +322,7 @@ inline bool set_cut(PagedAttn& p, int bm, int workers, int tile_cost, int snap, 
 }
 
 // A partial result: BM rows of d normalised sums, their maxima (times c, to base 2), their sums of weights beside those (apart, since the maximum
-// of very large scores would swallow the other's logarithm) and what rounding took from the maxima (see rest_of_product).  A worker leaves at most
+// of very large scores would swallow the other's logarithm) and what rounding took from large maxima (see rest_of_product).  A worker leaves at most
 // two: of the row tile that its run starts in, and of the one that it ends in.
 constexpr int64_t part_floats(int bm, int d) { return static_cast<int64_t>(bm) * (d + 3); }
 template <int BM, int D>

@@ -16,17 +16,21 @@ constexpr float kLeast = -3.0e38f;       // a running maximum before the first k
 __device__ __forceinline__ bool beyond_fma(float m) { return m != kLeast && __builtin_fabsf(m) > 0x1p29f; }
 
 // Sums with different references are joined by the references' difference.  A reference that is subtracted as the float it is needs nothing more; where
-// the scores were taken off the maximum m itself, the reference is m c without rounding: its float and, exactly, what rounding left of it.
-__device__ __forceinline__ float rest_of_product(float m, float c, float product) {
-  return __builtin_fabsf(product) < __builtin_inff() ? __builtin_fmaf(m, c, -product) : 0.f;
+// the scores were taken off the maximum m itself, the reference is m c without rounding: its float and, exactly, what rounding left of it.  Up to 2^30
+// that is at most 2^5, and the sums are multiplied by what it stands for; beyond, it goes along as the reference's rest, for joins whose largest reference
+// is beyond 2^29 (all others are so far above a reference with a rest that this has no weight).  m: m c afterwards; `times`: what to multiply the sums by.
+__device__ __forceinline__ float rest_of_product(float& m, float c, float& times) {
+  times = 1.f;
+  if (m == kLeast) return 0.f;
+  const float product = m * c, rest = __builtin_fabsf(product) < __builtin_inff() ? __builtin_fmaf(m, c, -product) : 0.f;
+  m = product;
+  if (__builtin_fabsf(product) > 0x1p30f) return rest;
+  times = fast_exp2(rest);
+  return 0.f;
 }
-struct Reference {
-  float m, rest;
-  // this less the other one, to 2^-24 of it: where the floats are near each other their difference is exact, and a rest is at most 2^-24 of its
-  // float, about as far as two scores of that size lie apart
-  __device__ __forceinline__ float less(const Reference& o) const { return (m - o.m) + (rest - o.rest); }
-  __device__ __forceinline__ Reference larger_of(const Reference& o) const { return o.less(*this) > 0.f ? o : *this; }
-};
+// One reference less another, to 2^-24 of it: where the floats are near each other their difference is exact, and a rest is at most 2^-24 of its float,
+// about as far as two scores of that size lie apart.
+__device__ __forceinline__ float less(float m, float rest, float of, float of_rest) { return (m - of) + (rest - of_rest); }
 
 // EL values from `col` on of the row (token, query head) at index rh, and its log-sum-exp (base 2; -inf: no key).
 template <int D, int EL>
@@ -63,35 +67,33 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
     const int here = min(sp.rows - m0, 16);                       // rows of this workgroup
     const int turns = here > 8 ? 1 : here > 4 ? 2 : here > 2 ? 4 : here > 1 ? 8 : 16, per_turn = 16 / turns;
     const int group = threadIdx.x / 16, je = threadIdx.x % 16 * EL, turn = group / per_turn, jr = first_row + min(group % per_turn, here - 1);
-    Reference top{kLeast, 0.f};
-    float total = 0.f, acc[EL];
+    float top = kLeast, top_rest = 0.f, total = 0.f, acc[EL];
 #pragma unroll
     for (int e = 0; e < EL; ++e) acc[e] = 0.f;
     // `N` parts from i0 on, every turns-th of them, all on their way at once
     auto add = [&](auto nn, int i0) __attribute__((always_inline)) {
       constexpr int N = decltype(nn)::value;
-      Reference m[N];
-      float l[N];
+      float m[N], l[N];
       f32x4 x[N][EL / 4];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int i = i0 + j * turns;
         const float* const src = part_of<BM, D>(p, i, i != worker);
-        m[j] = Reference{src[BM * D + jr], src[BM * D + 2 * BM + jr]};
+        m[j] = src[BM * D + jr];
         l[j] = src[BM * D + BM + jr];
 #pragma unroll
         for (int e = 0; e < EL / 4; ++e) x[j][e] = *reinterpret_cast<const f32x4*>(src + jr * D + je + 4 * e);
       }
-      Reference m_new = top;
+      float m_new = top;
 #pragma unroll
-      for (int j = 0; j < N; ++j) m_new = m_new.larger_of(m[j]);
-      const float a = fast_exp2(top.less(m_new));
+      for (int j = 0; j < N; ++j) m_new = fmaxf(m_new, m[j]);
+      const float a = fast_exp2(top - m_new);
       total *= a;
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] *= a;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float w = l[j] * fast_exp2(m[j].less(m_new));          // (parts without keys are zeros)
+        const float w = l[j] * fast_exp2(m[j] - m_new);          // (parts without keys are zeros)
         total += w;
 #pragma unroll
         for (int e = 0; e < EL; ++e) acc[e] += x[j][e / 4][e % 4] * w;
@@ -103,22 +105,21 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
     if (i + 3 * turns <= sp.last) { add(std::integral_constant<int, 4>{}, i); i += 4 * turns; }
     for (; i <= sp.last; i += turns) add(std::integral_constant<int, 1>{}, i);
     if (turns > 1) {                                              // (the same for the whole workgroup)
-      __shared__ float sums[16][D + 4], totals[16];
-      __shared__ Reference tops[16];
+      __shared__ float sums[16][D + 4], tops[16], totals[16];
 #pragma unroll
       for (int e = 0; e < EL; ++e) sums[group][je + e] = acc[e];
       if (je == 0) { tops[group] = top; totals[group] = total; }
       __syncthreads();
       if (turn > 0) return;                                       // (a row tile's last rows)
-      Reference m_new = top;
-      for (int t = 1; t < turns; ++t) m_new = m_new.larger_of(tops[t * per_turn + group]);
-      const float a = fast_exp2(top.less(m_new));
+      float m_new = top;
+      for (int t = 1; t < turns; ++t) m_new = fmaxf(m_new, tops[t * per_turn + group]);
+      const float a = fast_exp2(top - m_new);
       total *= a;
 #pragma unroll
       for (int e = 0; e < EL; ++e) acc[e] *= a;
       for (int t = 1; t < turns; ++t) {
         const int other = t * per_turn + group;
-        const float w = fast_exp2(tops[other].less(m_new));
+        const float w = fast_exp2(tops[other] - m_new);
         total += w * totals[other];
 #pragma unroll
         for (int e = 0; e < EL; ++e) acc[e] += w * sums[other][je + e];
@@ -127,11 +128,27 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedAttn p) {
     }
     const int m = m0 + group;
     if (group >= here) return;                                    // (so are these)
+    if (__builtin_expect(beyond_fma(top), 0)) {                   // once more, one part after the other, with the references' rests
+      top = kLeast; total = 0.f;
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] = 0.f;
+#pragma nounroll
+      for (int part = worker; part <= sp.last; ++part) {
+        const float* const src = part_of<BM, D>(p, part, part != worker);
+        const float m_part = src[BM * D + jr], rest = src[BM * D + 2 * BM + jr], gap = less(m_part, rest, top, top_rest);
+        const float a = gap > 0.f ? fast_exp2(-gap) : 1.f, w = src[BM * D + BM + jr] * (gap > 0.f ? 1.f : fast_exp2(gap));
+        total = total * a + w;
+#pragma unroll
+        for (int e = 0; e < EL; ++e) acc[e] = acc[e] * a + src[jr * D + je + e] * w;
+        top = gap > 0.f ? m_part : top;
+        top_rest = gap > 0.f ? rest : top_rest;
+      }
+    }
     const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int e = 0; e < EL; ++e) acc[e] *= inv;
     const int tok = divide(m, p.by_group);
-    store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, total == 0.f ? -__builtin_inff() : top.m + (top.rest + __builtin_amdgcn_logf(total)));
+    store_row<D, EL>(p, static_cast<int64_t>(sp.r0 + tok) * p.Hq + sp.head * p.G + (m - tok * p.G), je, acc, total == 0.f ? -__builtin_inff() : top + (top_rest + __builtin_amdgcn_logf(total)));
   }
 }
 

@@ -75,6 +75,28 @@ def test_large_scores_that_differ(tb, kv, low, high, hint):
 
 
 @pytest.mark.parametrize("hint", [1, 64])
+@pytest.mark.parametrize("kv,one,other", [(64, 5, 40), (64, 40, 5), (2000, 5, 1900), (9000, 8900, 100)])
+def test_equal_scores_beside_an_infinity(tb, kv, one, other, hint):
+    """Two keys of the same score, about 2^28 (base 2), of which one has a neighbour with an infinite value: only that one's wavefront or workgroup takes the
+    scores off its maximum before they are multiplied.  Both weigh the same, although rounding takes more than 2^3 from the product."""
+    page, d = 64, 64
+    c = np.float32(1.4426950408889634) / np.float32(8)
+    j = next(j for j in range(32) if abs(float(np.float32(2**31 + 256 * j) * c) - (2**31 + 256 * j) * float(c)) > 8)
+    n = -(-kv // page)
+    k = torch.zeros((n, 1, page, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.randn((n, 1, page, d), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    for t in (one, other):
+        k[t // page, 0, t % page, 0], k[t // page, 0, t % page, 1] = 2.0**15, 8.0 * j
+    v[(one + 1) // page, 0, (one + 1) % page, 9] = math.inf
+    q = torch.zeros((1, 2, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0], q[..., 1] = 2.0**16, 32.0
+    out, _ = tb.tasp_paged_attn(q, tb.PagedCache(k, v), _batch(tb, [list(range(n))], [kv], [0, 1], 1, hint), out_dtype=torch.float32)
+    rest = [x for x in range(d) if x != 9]
+    a, b = (v[t // page, 0, t % page].float() for t in (one, other))
+    assert ((out - (a + b) / 2).abs() <= 2.0**-18 * (a.abs() + b.abs()))[..., rest].all()
+
+
+@pytest.mark.parametrize("hint", [1, 64])
 @pytest.mark.parametrize("d", [64, 128])
 def test_scale_bytes_from_0_to_26(tb, d, hint):
     """Factors that the write never makes.  Byte 0 stands for 0 and the others for 2^(b - 127): read back exactly where the type holds the product; what they
