@@ -385,12 +385,14 @@ double tasp_chunk_attn_bwd_flops(const tasp_schedule_t* s, const tasp_attn_bwd_a
  *   page_table [n_seqs, max_pages]  position t lies in slot t % page_size of page page_table[b][t / page_size].
  *             An entry outside [0, n_pages) names no page: nothing is written there, rows read from there are
  *             0 and its keys are not visible.  So it is with positions below 0 or at and behind max_pages * page_size.
- *   max_rows  the most rows of any sequence, or 0 if it is not known: it decides only which kernel runs.
+ *   max_rows  the most rows of any sequence, or 0 if it is not known (then their mean counts).  A hint: it decides which
+ *             of two kernels tasp_paged_attn runs for the whole call, and with it how the probabilities are rounded.
  * Whatever the lists hold, no access leaves the buffers that the arguments describe: row_start is clipped to
  * [0, n_rows] and kv_len to at least 0.  Rows of the dense outputs outside
  * [row_start[0], row_start[n_seqs]) are left as they are.  A page may be in several tables (shared
  * prefixes); a position that two rows write in one call holds either, or parts of both.
- * max_pages * page_size <= 2^30, n_rows <= 2^30 (with tasp_paged_attn n_rows * Hq / Hkv <= 2^30).
+ * Limits: max_pages * page_size, n_rows * Hkv and n_seqs * Hkv at most 2^30, n_pages * Hkv * page_size below 2^32,
+ * Hkv * page_size * d below 2^30; with tasp_paged_attn also n_rows * Hq / Hkv and n_rows * Hq + 16 n_seqs * Hkv at most 2^30.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct tasp_paged_cache {
   void*    k;
@@ -418,7 +420,8 @@ int tasp_cache_write(const tasp_paged_cache* c, const tasp_paged_batch* b, const
                      int64_t k_stride, int64_t v_stride, int32_t dtype, void* hip_stream);
 
 /* The other way: every row of k and v (device, dense [n_rows, Hkv, d] of `dtype`) from its place in the
- * pages, times its scale.  Exact in both types. */
+ * pages, times its scale.  Exact in both types (bf16 rows with factors below 2^-124, which tasp_cache_write does not make:
+ * rounded to nearest even). */
 int tasp_cache_read(const tasp_paged_cache* c, const tasp_paged_batch* b, void* k, void* v, int32_t dtype,
                     void* hip_stream);
 
@@ -428,15 +431,19 @@ int tasp_cache_read(const tasp_paged_cache* c, const tasp_paged_batch* b, void* 
  *   out, lse  device, dense [n_rows, Hq, d] of out_dtype (bf16, or fp32 for a part that is merged) and [n_rows, Hq] fp32:
  *             as in tasp_chunk_attn.  A row that sees no key gets out = 0, lse = -inf.
  *   mask_mode TASP_MASK_CAUSAL: key t is visible to position p iff t <= p; TASP_MASK_FULL: every token of the sequence
- *             is (its kv_len may then be less than its rows, or 0).
+ *             is (its kv_len may then be less than its rows, or 0).  Positions are those in this cache: a window over a
+ *             sequence whose cache is spread over ranks cannot be expressed.
  *   window,   TASP_MASK_CAUSAL with window W > 0: of those keys the last W (t > p - W) and the first `sinks`
  *   sinks     (t < sinks).  0: all.
  *   softmax_scale  0 means 1/sqrt(d); otherwise positive and finite.
  *   workspace device, >= tasp_paged_attn_workspace_bytes() bytes, 256-byte aligned, caller-owned, contents undefined on
  *             entry and exit; calls that may overlap need one each.
- * Infinities and NaN in keys or values that a row does not see do not reach it.  K, V and P are multiplied in bf16
- * and summed in fp32.  The call only enqueues kernels on hip_stream and may be recorded into a graph; results
- * depend on the lists and inputs alone. */
+ * Infinities and NaN in keys or values that a row does not see do not reach it; those that it sees count as in the formula
+ * (0 times an infinity is NaN), and a row all of whose scores are -inf is as one that sees no key.
+ * Q, K and V are multiplied as bf16 and summed in fp32.  Probabilities enter the second product as two bf16 (together 2^-17
+ * of the value) where max_rows (or the mean) times Hq / Hkv is at most 32, and as one (2^-8) otherwise.
+ * The call only enqueues kernels on hip_stream and may be recorded into a graph.  The same call gives the same bits; the order of
+ * its sums goes by the lists, by n_rows, n_seqs, max_pages, max_rows and the other arguments, not by other work on the device. */
 typedef struct tasp_paged_attn_args {
   const void* q;
   void*       out;

@@ -498,7 +498,8 @@ class PagedCache:
 class PagedBatch:
     """Sequences of a PagedCache, as int32 device tensors that are read when a call runs: page_table [n_seqs, max_pages], kv_len [n_seqs]
     (tokens, the new rows included), row_start [n_seqs + 1] (first row of each sequence in the dense tensors).  n_rows: rows of the dense
-    tensors; max_rows: the most of any sequence, 0 if not known (a hint)."""
+    tensors; max_rows: the most of any sequence, 0 if not known (a hint: it decides which kernel PagedAttnPlan runs, and how that one rounds
+    probabilities)."""
 
     def __init__(self, page_table, kv_len, row_start, n_rows, max_rows=0):
         if page_table.dim() != 2 or tuple(kv_len.shape) != (page_table.shape[0],) or tuple(row_start.shape) != (page_table.shape[0] + 1,):
