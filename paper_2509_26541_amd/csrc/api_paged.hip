@@ -58,8 +58,9 @@ bool rows_type(int32_t dtype) { return dtype == TASP_DTYPE_FP32 || dtype == TASP
 int status_of(hipError_t e) { return e == hipSuccess ? TASP_OK : TASP_EHIP; }
 
 // Rows (token, query head of the group) of a sequence and KV head, by the hint or the mean.  Up to kFew the kernel for few of them takes the call: it
-// keeps more loads on their way, and its wavefronts all have work.  32 sequences of 16 000 tokens, 8 KV heads of 128: 32 rows e4m3 192 us with it,
-// 244 with the other, bf16 320 and 365; 64 rows (it would walk the keys twice) 394 and 250.
+// keeps more loads on their way, and its wavefronts all have work.  32 sequences of 16 000 tokens, 8 KV heads of 128: 32 rows e4m3 209 us with it,
+// 241 with the other, bf16 323 and 365; 64 rows (it would walk the keys twice) e4m3 342 and 277, bf16 504 and 374.  A call runs one kernel for all of its
+// sequences: 63 single tokens of 1 000 to 32 000 with a chunk of 2 048 of 16 384 take 857 us e4m3 and 811 bf16, apart 209 + 530 and 399 + 497.
 constexpr int64_t kFew = 32;
 int64_t rows_of(const tasp::PagedAttn& p, const tasp_paged_batch* b) {
   return (b->max_rows > 0 ? b->max_rows : (b->n_rows + larger(b->n_seqs, 1) - 1) / larger(b->n_seqs, 1)) * p.G;

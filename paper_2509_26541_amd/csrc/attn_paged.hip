@@ -3,9 +3,9 @@
 // S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, softmax in one pass (running maximum and sum).  A grouped head's K and V
 // are read once for all 16 rows.  Every wavefront takes keys of its own, in stages of 32, through a part of LDS of its own that loads
 // fill directly: no barrier inside the loop, and the loads run ahead of the products by the stages behind the first.
-// What bounds it is HBM: per key and KV head 4 d bytes (e4m3: 2 d + 2) for 4 d 16 products.  One token of 512 000, 8 KV heads of 128: 311 us,
-// 6.6 TB/s of 7.0 that a kernel that only reads gets (e4m3 half of it, 5.9); 64 sequences of e4m3 196 us, 6.1 TB/s.  One token of 700 is latency:
-// 6.6 us, and 2.8 for the joining kernel.
+// What bounds it is HBM: per key and KV head 4 d bytes (e4m3: 2 d + 2) for 4 d 16 products.  One token of 500 003, 8 KV heads of 128: 312 us,
+// 6.6 TB/s of 7.0 that a kernel that only reads gets; 64 sequences of e4m3, 1 000 to 32 000 tokens, 193 us, 6.2 TB/s.  One token of 700 is latency:
+// 6.5 us, and 3.2 for the joining kernel.
 //
 // The work of a call (sequence after sequence, KV head after KV head, row tile after row tile, in key tiles) is cut into equal runs,
 // one for a workgroup; where a run ends inside a row tile, partial results go to the workspace and paged_combine_kernel adds them up,
@@ -449,9 +449,11 @@ __global__ __launch_bounds__((RowsCfg<D, F8, NR>::NW * 64), (RowsCfg<D, F8, NR>:
   leave_split(p, worker, split);
 }
 
-// Beside its keys a row tile counts as 64 of them; 16 or more are split off one, and a run has at least 64.  18 calls of 1 to 512 sequences and 1 to
-// 512 000 tokens, geometric mean: 64, 16, 64 (tile, split, run) 38.3 us; 16, 16, 64 38.8 (64 sequences of e4m3 203 us for 200); 128, 32, 128 39.1;
-// 192, 64, 256 41.0 (one token of 700: 12.1 for 9.7).
+// Beside its keys a row tile counts as 64 of them; 16 or more are split off one, and a run has at least 64.  18 calls, geometric mean: 64, 16, 64
+// (tile, split, run) 38.4 us; 16, 16, 64 39.2 (64 sequences of e4m3 202 us for 198); 128, 32, 128 39.4; 192, 64, 256 41.3 (one token of 700: 12.1 for
+// 9.7).  They are the four cases of perf/operators.py that come here; of its default heads (32 over 8 of 128, bf16 unless said) one token for 8 sequences of
+// 300 keys, 1 of 4 000, 32 of 100 to 900 e4m3, 16 of 2 000 e4m3, 4 of 30 000 and 128 of 500 to 1 500; and the first 8 calls of attention with
+// at most 32 rows that its draw() gives from random.Random(3).
 template <int D, bool F8, int NR>
 bool cut(PagedAttn& p) { return set_cut(p, 16 * NR, 256 * RowsCfg<D, F8, NR>::PER_CU, 64, 16, 64); }
 

@@ -6,8 +6,12 @@
 // descriptor is made of it by scalar instructions (base, and how many bytes of the 16 rows count: what lies behind, and pages that
 // do not exist, come as zeros).  e4m3 rows are loaded into registers a tile ahead, widened (times their scale, exactly) and written to LDS as bf16.
 //
-// What bounds it: vector issue, as in attn_run.hip.  2 048 new tokens of 64 000, 32 and 8 heads of 128: 1.94 ms, 1.11 PFLOP/s (a large matrix
-// product reaches 1.375 on this card).  Few rows of long e4m3 sequences are bound by latency (48 rows, 226 us for 109 of reading).
+// What bounds it: vector issue, as in attn_run.hip.  2 048 new tokens of 65 536, 32 and 8 heads of 128: 1.93 ms, 1.12 PFLOP/s (a large matrix
+// product reaches 1.375 on this card).  Few rows of long e4m3 sequences are bound by latency (48 rows, 229 us for 109 of reading).
+//
+// Rounding: P goes into the second product as one bf16, off by at most 2^-8 of its value, as in the kernels of dense K and V; the largest
+// probability of a tile is taken as it was rounded in the sum that the output is divided by.  A second bf16 for what rounding left, as in the kernel for few rows,
+// would be half as many matrix instructions again, beside a pipe that is 60 % busy, and as many vector instructions to make it, which are the bound.
 //
 // The work of a call is cut into equal runs, one for a workgroup (PagedRun), as in attn_paged.hip.
 #include <hip/hip_runtime.h>
@@ -610,7 +614,7 @@ __global__ __launch_bounds__((PTileCfg<D, F8>::NTHREADS), (D == 64 && !F8 ? 3 : 
 }
 
 // Three and two workgroups to a CU.  Beside its keys a row tile costs as much as 512 of them, and less than 512 are not split off one: a partial result
-// is as dear (12 ragged chunks of up to 1 500 new tokens: 121 us, 137 with 128 and 256; a window of 2 048 at d = 64: 109 and 113).
+// is as dear (12 ragged chunks of up to 1 500 new tokens: 114 us, 129 with 128 and 256; a window of 2 048 at d = 64: 109 and 112).
 bool cut(PagedAttn& p, bool e4m3, int d) { return set_cut(p, 128, d == 64 && !e4m3 ? 768 : 512, 512, 512, 512); }
 
 template <int D, bool F8>

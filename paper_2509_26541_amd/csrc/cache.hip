@@ -2,7 +2,7 @@
 //
 // A (token, KV head) pair is d consecutive values on both sides, so both kernels are streams of 16-byte pieces with the pages looked
 // up on the way; what bounds them is HBM (few tokens: three dependent loads, the sequence, its page, the row: 1.9 us for one token).  Prompts of
-// bf16 into e4m3 pages 91 us, 4.6 TB/s; back 84 us, 5.2 TB/s; a large copy reaches 4.9 on this card.
+// bf16 into e4m3 pages (68 859 tokens of 8 heads of 128) 92 us, 4.6 TB/s; 71 691 back 85 us, 5.2 TB/s; a large copy reaches 4.9 on this card.
 // e4m3 rows have one scale, a power of two: the smallest with which the row's largest finite magnitude is at most 448.  Dividing by
 // it is exact, so each value is rounded once, and value times scale is exact in bf16 (4 bits and 8 of exponent).
 #include <hip/hip_runtime.h>
@@ -49,9 +49,10 @@ __device__ __forceinline__ void load_once(const T* p, T (&x)[N]) {
 }
 
 // A lane has eight values of a row, D / 8 neighbouring lanes the whole of it: 16-byte pieces of bf16 that lie side by side.  A wavefront has 512 / D
-// tokens and HEADS of their KV heads, so that what it has looked up serves more bytes.  Writing 68 859 tokens of 8 heads of 128 as e4m3: 85 us
-// with four heads (5.0 TB/s, a copy's rate), 96 with one; reading 71 691: 85 and 113.  With sixteen values to a lane, 16 bytes of e4m3: 86 and 98,
-// and 193 instead of 141 from fp32 rows, whose pieces do not lie side by side then.
+// tokens and HEADS of their KV heads, so that what it has looked up serves more bytes.  The same calls on two inputs in turn (a part of which the
+// caches then hold): writing e4m3 86 us with four heads, 98 with one, reading 86 and 108; from fp32 rows 141 and 148; bf16 pages, where the bytes
+// outweigh the look-up, 111 and 109, 107 and 103.  With sixteen values to a lane, 16 bytes of e4m3: writing 86, reading 98, and 194 from fp32 rows,
+// whose pieces do not lie side by side then.
 constexpr int kPiece = 8;
 template <int D>
 constexpr int kTokens = 64 * kPiece / D;
