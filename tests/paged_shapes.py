@@ -13,7 +13,7 @@ ROWS = {("bf16", 128, 2): 512, ("bf16", 128, 4): 512, ("e4m3", 128, 2): 1024, ("
 TILES = {("bf16", 128, 5): 512, ("e4m3", 128, 5): 512, ("bf16", 64, 5): 768, ("e4m3", 64, 5): 512}
 
 
-def batch(kind, d, tokens, windowed):
+def batch(kind, d, tokens):
     """(new tokens, tokens in all) of every sequence: long ones, so many that a workgroup's share is some 270 tiles (kernel for few rows) or 140, and,
     for the kernel for many rows, shorter ones that are not split."""
     rng = random.Random(1000 * d + 10 * tokens + (kind == "e4m3"))

@@ -100,7 +100,7 @@ def _queries(k, table, kv, starts, hq, seed):
 def test_long_runs(tb, kind, d, tokens, windowed):
     """Pieces of more than 256 key tiles (few rows) and 128 (many); then with a column of V that is not finite in a few pages, so that sums are formed again by
     the pass for such values, over all tiles."""
-    new, kv = paged_shapes.batch(kind, d, tokens, windowed)
+    new, kv = paged_shapes.batch(kind, d, tokens)
     starts = np.concatenate([[0], np.cumsum(new)]).tolist()
     table = paged_shapes.table(kv, d + tokens)
     hkv, hq = paged_shapes.HKV, paged_shapes.HKV * paged_shapes.GROUP

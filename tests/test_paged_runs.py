@@ -81,7 +81,7 @@ def _cut_constants(few):
 def _pieces(exe, kind, d, tokens, windowed):
     few = (kind, d, tokens) in paged_shapes.ROWS
     workers = (paged_shapes.ROWS if few else paged_shapes.TILES)[kind, d, tokens]
-    new, kv = paged_shapes.batch(kind, d, tokens, windowed)
+    new, kv = paged_shapes.batch(kind, d, tokens)
     bm, width = (8 * tokens if few else 128), max(-(-x // paged_shapes.PAGE) for x in kv)
     head = [bm, workers, *_cut_constants(few), len(kv), paged_shapes.HKV, paged_shapes.GROUP, 1 if windowed else 0, paged_shapes.WINDOW if windowed else 0,
             paged_shapes.SINKS if windowed else 0, width]
